@@ -62,6 +62,18 @@ enum scone_placement {
     SCONE_PLACE_HOST = 1   /* `rows` is host-mapped pinned memory, read over PCIe */
 };
 
+enum scone_type {
+    SCONE_BF16 = 0,
+    SCONE_FP16 = 1,
+    SCONE_FP32 = 2,
+    SCONE_MX4 = 3  /* 4-bit rows, see scone_quantize_mx4 */
+};
+
+enum scone_activation {
+    SCONE_ACT_NONE = 0,
+    SCONE_ACT_GELU = 1     /* x Phi(x), not the tanh form */
+};
+
 #define SCONE_MAX_FGRAM_LEN 7     /* longest f-gram a table can hold */
 #define SCONE_TOKEN_LIMIT 65536   /* tokens are packed as 16-bit fields */
 
@@ -357,6 +369,106 @@ int64_t scone_gather_split_workspace(int64_t n_tok, int64_t row_bytes);
 int scone_gather_split_static(const int32_t* fgram_ids, int64_t n_tok, const void* near_rows,
                               int64_t n_near, const void* far_rows, int64_t n_far,
                               int64_t row_bytes, void* out, int32_t* n_unique, void* stream);
+
+/*
+ * Rows in 4 bits (microscaled 4-bit floating point: the E2M1 elements and E8M0
+ * scales of the OCP Microscaling Formats specification, in blocks of 32).  A
+ * table of them takes 0.27 times the memory of bf16 rows, and a gather over PCIe
+ * or from HBM moves that much less.
+ *
+ * A row of `cols` elements (1 <= cols <= 2^22) has g = ceil(cols / 128) groups:
+ * 64 g bytes of codes, element 2 i in the low half of byte i and 2 i + 1 in the
+ * high half, then 4 g scale bytes, one per 32 elements, then zeros up to a multiple
+ * of 16 bytes.  Codes past `cols` and the scale bytes of blocks past it are 0.  A
+ * code holds a sign (bit 3) and a magnitude, {0, 1/2, 1, 3/2, 2, 3, 4, 6}[code & 7];
+ * its value is that times 2^(s - 127), s the scale byte.  s = 255 makes the block NaN.
+ *
+ * scone_mx4_row_bytes: the bytes of such a row, or -1 for cols outside the range.
+ * A 4-bit table is a table of rows of that many bytes for every call that moves
+ * rows as bytes (scone_gather, scone_embed, scone_gather_split, ...).
+ */
+int64_t scone_mx4_row_bytes(int64_t cols);
+
+/*
+ * Quantisation of rows: rows[r] = the 4-bit row of x[r, 0..cols).  Each block of 32
+ * elements gets the scale 2^(floor(log2 m) - 2), m its largest magnitude (at least
+ * 2^-127; that for a block of zeros), and each element is divided by it and rounded to
+ * the nearest code, ties to the even one, magnitudes above 6 to 6.  A block that holds
+ * an infinity or a NaN gets the scale byte 255 and codes 0: it reads as NaN.
+ *
+ *  x        [n_rows, cols] of x_type (SCONE_BF16, SCONE_FP16 or SCONE_FP32), row r
+ *           at element r * ld, ld >= cols; aligned to its elements.
+ *  rows     [n_rows, scone_mx4_row_bytes(cols)] device output, 16-byte aligned;
+ *           sharing memory with x gives SCONE_EINVAL.
+ *
+ * Asynchronous on `stream`.  n_rows = 0 launches nothing.
+ */
+int scone_quantize_mx4(const void* x, int32_t x_type, int64_t n_rows, int64_t cols, int64_t ld,
+                       void* rows, void* stream);
+
+/*
+ * scone_gather over a 4-bit table: out[k, :] = the values of rows[fgram_ids[k], :],
+ * rounded to out_type where it cannot hold them (bf16 and fp32 hold every value of a
+ * row that scone_quantize_mx4 wrote).
+ *
+ *  fgram_ids  [n_tok] int32, as for scone_gather (an id outside [0, n_rows) gives
+ *             SCONE_EROW via scone_check and a row of zeros); or NULL for the rows
+ *             0 .. n_tok - 1 in order (n_tok > n_rows is then SCONE_EINVAL).
+ *  rows       [n_rows, scone_mx4_row_bytes(cols)], 16-byte aligned, in device memory
+ *             or host-mapped (placement).
+ *  out        [n_tok, cols] device output of out_type (SCONE_BF16, SCONE_FP16 or
+ *             SCONE_FP32), aligned to its elements; sharing memory with `rows` or
+ *             with fgram_ids gives SCONE_EINVAL.
+ *
+ * Asynchronous on `stream`.  n_tok = 0 launches nothing.
+ */
+int scone_gather_mx4(const int32_t* fgram_ids, int64_t n_tok, const void* rows, int64_t n_rows,
+                     int64_t cols, void* out, int32_t out_type, int32_t placement, void* stream);
+
+/*
+ * scone_decode_step over a 4-bit table: the same step, with the values of the row
+ * in `out`, [S, cols] of out_type.  rows, cols, out and out_type as for
+ * scone_gather_mx4, everything else as for scone_decode_step.
+ */
+int scone_decode_step_mx4(const scone_table_t* table, int32_t* ctx, int32_t* ctx_len,
+                          int32_t ctx_cap, const int32_t* new_tok, int64_t S, int32_t max_n,
+                          const void* rows, int64_t n_rows, int64_t cols, int32_t placement,
+                          void* out, int32_t out_type, int32_t* fgram_ids, int8_t* match_len,
+                          void* stream);
+
+/*
+ * Linear map with 4-bit weights and activations (scone_quantize_mx4 has the format):
+ *     out[m, n] = act(sum_k x[m, k] w[n, k] + bias[n]) + residual[m, n]
+ * x is given in 4 bits, or quantised as scone_quantize_mx4 does by the call.  Products
+ * are exact, sums and the rest fp32, rounded once to out_type.
+ *
+ *  x          [M, K] of x_type: SCONE_BF16, SCONE_FP16 or SCONE_FP32 with row m at
+ *             element m * ld_x (ld_x >= K, at most 2^28), aligned to its elements; or
+ *             SCONE_MX4, rows of scone_mx4_row_bytes(K) bytes, 16-byte aligned
+ *             (ld_x is then ignored).
+ *  w          [N, scone_mx4_row_bytes(K)] 4-bit rows, one per output, 16-byte aligned.
+ *  M, N       below 2^31; K in [1, 2^22].
+ *  bias       [N] of bias_type (SCONE_BF16, SCONE_FP16 or SCONE_FP32), or NULL.
+ *  activation SCONE_ACT_NONE or SCONE_ACT_GELU.
+ *  residual   [M, N] of out_type, row m at element m * ld_out, or NULL; it may be
+ *             `out` itself, which is then added to.
+ *  out        [M, N] of out_type, row m at element m * ld_out (ld_out >= N, at most
+ *             2^28), aligned to its elements; elements between rows stay as they are.
+ *  workspace  device scratch of at least scone_linear_mx4_workspace bytes, 16-byte
+ *             aligned (else SCONE_EINVAL), caller-owned, reusable across calls that do
+ *             not overlap; NULL where that is 0.
+ *
+ * out may share memory with nothing that is read (but a residual that is out), nor the
+ * workspace with anything (SCONE_EINVAL).  Asynchronous on `stream`; launches kernels
+ * only.  M * N = 0 launches nothing.
+ */
+int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int64_t M, int64_t K,
+                     const void* w, int64_t N, const void* bias, int32_t bias_type,
+                     int32_t activation, const void* residual, void* out, int32_t out_type,
+                     int64_t ld_out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace scone_linear_mx4 needs, or -1 for sizes or types it rejects. */
+int64_t scone_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, int32_t x_type);
 
 /*
  * F-gram discovery (Algorithm 3: count every n-gram, n = 2..max_len, of all

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 import threading
 from typing import Optional, Tuple
@@ -22,6 +23,8 @@ LIB_PATH = os.path.join(_PKG, "libscone.so")
 OK, EINVAL, ELEN, EID, EDUP, EFULL, ENOMEM, EHIP, ETOKEN, EROW, ESCRATCH = range(11)
 SPLIT_STATIC_BYTES = 32 << 20   # scone_gather_split_static's scratch (SCONE_SPLIT_STATIC_BYTES)
 PLACE_HBM, PLACE_HOST = 0, 1
+BF16, FP16, FP32, MX4 = range(4)    # scone_type
+ACT_NONE, ACT_GELU = 0, 1           # scone_activation
 MAX_FGRAM_LEN = 7
 TOKEN_LIMIT = 65536
 
@@ -86,6 +89,20 @@ def _declare(L):
     L.scone_fgram_model_layout.argtypes = [I32, I32, I32, I32, I32, ctypes.POINTER(I64),
                                            ctypes.POINTER(I64), ctypes.POINTER(I64)]
     L.scone_fgram_model_layout.restype = I
+    L.scone_mx4_row_bytes.argtypes = [I64]
+    L.scone_mx4_row_bytes.restype = I64
+    L.scone_quantize_mx4.argtypes = [P, I32, I64, I64, I64, P, P]
+    L.scone_quantize_mx4.restype = I
+    L.scone_gather_mx4.argtypes = [P, I64, P, I64, I64, P, I32, I32, P]
+    L.scone_gather_mx4.restype = I
+    L.scone_decode_step_mx4.argtypes = [P, P, P, I32, P, I64, I32, P, I64, I64, I32, P, I32, P,
+                                        P, P]
+    L.scone_decode_step_mx4.restype = I
+    L.scone_linear_mx4.argtypes = [P, I32, I64, I64, I64, P, I64, P, I32, I32, P, P, I32, I64, P,
+                                   I64, P]
+    L.scone_linear_mx4.restype = I
+    L.scone_linear_mx4_workspace.argtypes = [I64, I64, I64, I32]
+    L.scone_linear_mx4_workspace.restype = I64
     L.scone_host_alloc.argtypes = [I64, ctypes.POINTER(P), ctypes.POINTER(P)]
     L.scone_host_alloc.restype = I
     L.scone_host_free.argtypes = [P]
@@ -629,6 +646,263 @@ def gather_split(fgram_ids: torch.Tensor, near_rows: torch.Tensor, far_rows: "Ho
                                       _ptr(n_unique), _stream(stream))
     _check(rc, "scone_gather_split")
     return out
+
+
+# ------------------------------------------------------------- 4-bit rows ----
+
+_TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
+
+
+def mx4_row_bytes(cols: int) -> int:
+    """Bytes of a 4-bit row of `cols` elements (scone_mx4_row_bytes)."""
+    n = int(lib().scone_mx4_row_bytes(int(cols)))
+    if n < 0:
+        raise ValueError("cols must be in [1, 2^22]")
+    return n
+
+
+class Mx4Rows:
+    """A table of 4-bit rows of `cols` elements: microscaled E2M1 codes and their
+    scales, mx4_row_bytes(cols) bytes per row (include/scone.h has the layout).
+
+    ``data`` is a contiguous CUDA uint8 tensor [n_rows, mx4_row_bytes(cols)], or a
+    HostRows of such rows in pinned host memory.  The calls that move rows as bytes
+    (gather, embed, gather_split, ...) take ``data``."""
+
+    def __init__(self, data, cols: int):
+        self.cols = int(cols)
+        self.row_bytes = mx4_row_bytes(self.cols)
+        placement, ptr, n_rows, row_bytes, row_shape, dtype = _rows_arg(data)
+        if dtype != torch.uint8 or row_shape != (self.row_bytes,):
+            raise ValueError(f"data must be uint8 rows of {self.row_bytes} bytes")
+        if ptr is not None and ptr % 16:
+            raise ValueError("data must be 16-byte aligned")
+        self.data = data
+        self.placement, self.n_rows = placement, n_rows
+
+    @property
+    def device(self) -> Optional[torch.device]:
+        """The tensor's device; None for rows in host memory."""
+        return self.data.device if self.placement == PLACE_HBM else None
+
+    @property
+    def nbytes(self) -> int:
+        return self.n_rows * self.row_bytes
+
+    @property
+    def ptr(self) -> Optional[int]:
+        return _ptr(self.data) if self.placement == PLACE_HBM else self.data.device_ptr
+
+
+def _mx4_arg(rows, name: str, device: Optional[torch.device] = None) -> Mx4Rows:
+    if not isinstance(rows, Mx4Rows):
+        raise TypeError(f"{name} must be Mx4Rows")
+    if device is not None and rows.device is not None and rows.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    return rows
+
+
+def _float_type(dtype, name: str) -> int:
+    if dtype not in _TYPES:
+        raise TypeError(f"{name} must be bfloat16, float16 or float32, got {dtype}")
+    return _TYPES[dtype]
+
+
+def _float_matrix(x, name: str) -> int:
+    """The row stride of a CUDA float matrix whose rows are contiguous."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    _float_type(x.dtype, name)
+    if x.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions")
+    n, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if n > 1 and x.stride(0) < cols:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return x.stride(0) if n > 1 else max(cols, 1)
+
+
+def quantize_mx4(x: torch.Tensor, out: Optional[Mx4Rows] = None, stream=None) -> Mx4Rows:
+    """scone_quantize_mx4: the rows of x [n, cols] (bfloat16, float16 or float32, any
+    row stride) in 4 bits."""
+    ld = _float_matrix(x, "x")
+    n, cols = x.shape
+    if out is None:
+        out = Mx4Rows(torch.empty((n, mx4_row_bytes(cols)), dtype=torch.uint8, device=x.device),
+                      cols)
+    _mx4_arg(out, "out", x.device)
+    if out.placement != PLACE_HBM or out.n_rows != n or out.cols != cols:
+        raise ValueError("out must be device rows of x's shape")
+    with _on(x.device):
+        rc = lib().scone_quantize_mx4(_ptr(x), _TYPES[x.dtype], n, cols, ld, out.ptr,
+                                      _stream(stream))
+    _check(rc, "scone_quantize_mx4")
+    return out
+
+
+def gather_mx4(fgram_ids: Optional[torch.Tensor], rows: Mx4Rows,
+               dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """scone_gather_mx4: out[k] = the values of rows[fgram_ids[k]] in `dtype` (that of
+    `out` when given)."""
+    _dev_i32(fgram_ids, "fgram_ids")
+    return _gather_mx4(fgram_ids, tuple(fgram_ids.shape), fgram_ids.device, rows, dtype, out,
+                       stream)
+
+
+def dequantize_mx4(rows: Mx4Rows, dtype: torch.dtype = torch.bfloat16,
+                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values of all rows, [n_rows, cols] (scone_gather_mx4 without ids).  Rows in
+    host memory are read by the current device."""
+    _mx4_arg(rows, "rows")
+    device = rows.device if rows.device is not None else \
+        torch.device("cuda", torch.cuda.current_device())
+    return _gather_mx4(None, (rows.n_rows,), device, rows, dtype, out, stream)
+
+
+def _gather_mx4(ids, shape, device, rows, dtype, out, stream):
+    _mx4_arg(rows, "rows", device)
+    if out is None:
+        _float_type(dtype, "dtype")
+        out = torch.empty(shape + (rows.cols,), dtype=dtype, device=device)
+    else:
+        dtype = out.dtype
+        _float_type(dtype, "out")
+        if out.device != device:
+            raise ValueError(f"out must be on {device}")
+    n_tok = math.prod(shape)
+    if not out.is_contiguous() or out.numel() != n_tok * rows.cols:
+        raise ValueError("out must be contiguous with n_tok * cols elements")
+    with _on(device):
+        rc = lib().scone_gather_mx4(_ptr(ids), n_tok, rows.ptr, rows.n_rows, rows.cols, _ptr(out),
+                                    _TYPES[dtype], rows.placement, _stream(stream))
+    _check(rc, "scone_gather_mx4")
+    return out
+
+
+def decode_step_mx4(table: Table, ctx: torch.Tensor, ctx_len: torch.Tensor, new_tok: torch.Tensor,
+                    max_n: int, rows: Mx4Rows, out: torch.Tensor,
+                    fgram_ids: Optional[torch.Tensor] = None,
+                    match_len: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """scone_decode_step_mx4: decode_step over a 4-bit table, the rows' values in
+    out [S, cols] (bfloat16, float16 or float32)."""
+    _dev_i32(ctx, "ctx", 2)
+    _dev_i32(ctx_len, "ctx_len", 1)
+    _dev_i32(new_tok, "new_tok", 1)
+    S, cap = ctx.shape
+    if ctx_len.numel() != S or new_tok.numel() != S:
+        raise ValueError("ctx, ctx_len and new_tok disagree on S")
+    dev = ctx.device
+    _mx4_arg(rows, "rows", dev)
+    out_type = _float_type(out.dtype, "out")
+    if not out.is_contiguous() or out.numel() != S * rows.cols:
+        raise ValueError("out must be contiguous with S * cols elements")
+    if ctx_len.device != dev or new_tok.device != dev or out.device != dev:
+        raise ValueError(f"ctx_len, new_tok and out must be on {dev}")
+    for name, t, dt in (("fgram_ids", fgram_ids, torch.int32), ("match_len", match_len, torch.int8)):
+        if t is not None and (t.dtype != dt or t.numel() != S or not t.is_contiguous()
+                              or t.device != dev):
+            raise ValueError(f"{name} must be a contiguous {dt} tensor of S elements on {dev}")
+    with _on(dev):
+        rc = lib().scone_decode_step_mx4(table.handle, _ptr(ctx), _ptr(ctx_len), cap,
+                                         _ptr(new_tok), S, int(max_n), rows.ptr, rows.n_rows,
+                                         rows.cols, rows.placement, _ptr(out), out_type,
+                                         _ptr(fgram_ids), _ptr(match_len), _stream(stream))
+    _check(rc, "scone_decode_step_mx4")
+    return out
+
+
+def linear_mx4_workspace_bytes(M: int, N: int, K: int, dtype=None) -> int:
+    """Bytes of scratch scone_linear_mx4 needs for an x of `dtype` (None: 4-bit rows)."""
+    x_type = MX4 if dtype is None else _float_type(dtype, "dtype")
+    n = int(lib().scone_linear_mx4_workspace(int(M), int(N), int(K), x_type))
+    if n < 0:
+        raise ValueError("invalid sizes")
+    return n
+
+
+def linear_mx4(x, w: Mx4Rows, bias: Optional[torch.Tensor] = None, gelu: bool = False,
+               residual: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """scone_linear_mx4: act(x w^T + bias) + residual for x [..., K] (bfloat16, float16
+    or float32, quantised by the call) or 4-bit rows [M, K] (Mx4Rows), and w [N, K] in
+    4 bits.  The result is [..., N] of `dtype` (default: x's, bfloat16 for 4-bit rows),
+    or `out`, which may be a matrix with strided rows and may be the residual itself.
+    `residual` has the result's shape, type and row stride.  The scratch is
+    `workspace` (a CUDA uint8 tensor of linear_mx4_workspace_bytes) or, when None, a
+    tensor from torch's caching allocator."""
+    _mx4_arg(w, "w")
+    if w.placement != PLACE_HBM:
+        raise ValueError("w must be device rows")
+    dev, N, K = w.device, w.n_rows, w.cols
+    if isinstance(x, Mx4Rows):
+        _mx4_arg(x, "x", dev)
+        if x.placement != PLACE_HBM:
+            raise ValueError("x must be device rows")
+        M, Kx, lead, x_type, ld_x, x_ptr = x.n_rows, x.cols, (x.n_rows,), MX4, 0, x.ptr
+        dtype = torch.bfloat16 if dtype is None else dtype
+    else:
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise TypeError("x must be a CUDA (HIP) tensor or Mx4Rows")
+        if x.dim() < 1:
+            raise ValueError("x must have at least one dimension")
+        lead, Kx = tuple(x.shape[:-1]), x.shape[-1]
+        if x.dim() != 2 and not x.is_contiguous():
+            raise ValueError("x must be contiguous, or a matrix with contiguous rows")
+        x2 = x if x.dim() == 2 else x.view(math.prod(lead), Kx)
+        ld_x = _float_matrix(x2, "x")
+        M, x_type, x_ptr = x2.shape[0], _TYPES[x.dtype], _ptr(x2)
+        dtype = x.dtype if dtype is None else dtype
+        if x.device != dev:
+            raise ValueError(f"x must be on {dev}")
+    if Kx != K:
+        raise ValueError(f"x has rows of {Kx} elements, w of {K}")
+    if out is None:
+        _float_type(dtype, "dtype")
+        out = torch.empty(lead + (N,), dtype=dtype, device=dev)
+    if out.device != dev or tuple(out.shape) != lead + (N,):
+        raise ValueError(f"out must be [..., {N}] on {dev}")
+    out_type = _float_type(out.dtype, "out")
+    ld_out = _row_stride(out, M, N, "out")
+    if residual is not None:
+        if residual.dtype != out.dtype or residual.shape != out.shape or residual.device != dev:
+            raise ValueError("residual must have the result's shape, type and device")
+        if M > 1 and N > 0 and _row_stride(residual, M, N, "residual") != ld_out:
+            raise ValueError("residual must have the result's row stride")
+        _row_stride(residual, M, N, "residual")
+    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.device != dev
+                             or tuple(bias.shape) != (N,) or not bias.is_contiguous()):
+        raise ValueError(f"bias must be a contiguous tensor of {N} elements on {dev}")
+    bias_type = BF16 if bias is None else _float_type(bias.dtype, "bias")
+    with _on(dev):
+        need = lib().scone_linear_mx4_workspace(M, N, K, x_type)
+        if workspace is None:
+            if need > 0:
+                workspace = _scratch(need, dev, stream)
+                if workspace is None:
+                    raise SconeError(ENOMEM, "scone_linear_mx4")
+        elif workspace.dtype != torch.uint8 or workspace.device != dev \
+                or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+        rc = lib().scone_linear_mx4(
+            x_ptr, x_type, ld_x, M, K, w.ptr, N, _ptr(bias), bias_type,
+            ACT_GELU if gelu else ACT_NONE, _ptr(residual), _ptr(out), out_type, ld_out,
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+    _check(rc, "scone_linear_mx4")
+    return out
+
+
+def _row_stride(t: torch.Tensor, M: int, N: int, name: str) -> int:
+    """The row stride of a result [..., N] of M rows: any for a matrix, N otherwise."""
+    if t.dim() == 2 and M > 1 and N > 0:
+        if (N > 1 and t.stride(1) != 1) or t.stride(0) < N:
+            raise ValueError(f"{name} must have contiguous rows that do not overlap")
+        return t.stride(0)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, or a matrix with contiguous rows")
+    return N
 
 
 def check(stream=None, device=None) -> int:
