@@ -34,6 +34,7 @@
 // bandwidth-bound and one wavefront handles one row or one f-gram.
 #include "fgram_tree.h"
 #include "gemm_bf16.h"
+#include "gemm_mx4.h"
 
 #include <algorithm>
 #include <new>
@@ -573,4 +574,79 @@ extern "C" int scone_fgram_model_forward(const int32_t* fgrams, const int32_t* l
     return scone_fgram_model_forward_in(fgrams, lengths, row_ids, n, max_len, tok_rows, vocab,
                                         params, d, n_heads, d_ff, n_layers, rows, n_rows, nullptr,
                                         0, stream);
+}
+
+// ---------------------------------------------------- the 4-bit linear map --
+
+namespace scone {
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 31;
+
+bool sizes_ok(int64_t M, int64_t N, int64_t K) {
+    return M >= 0 && N >= 0 && M < kMaxRows && N < kMaxRows && mx4::cols_ok(K);
+}
+
+// 4-bit rows of x, where the call makes them.
+int64_t workspace_bytes_for(int64_t M, int64_t K, int32_t x_type) {
+    return x_type == SCONE_MX4 ? 0 : M * mx4::row_bytes(K);
+}
+
+}  // namespace
+}  // namespace scone
+
+extern "C" int64_t scone_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, int32_t x_type) {
+    using namespace scone;
+    if (!sizes_ok(M, N, K) || (x_type != SCONE_MX4 && mx4::elem_bytes(x_type) == 0)) return -1;
+    return N == 0 ? 0 : workspace_bytes_for(M, K, x_type);
+}
+
+extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int64_t M, int64_t K,
+                                const void* w, int64_t N, const void* bias, int32_t bias_type,
+                                int32_t activation, const void* residual, void* out,
+                                int32_t out_type, int64_t ld_out, void* workspace,
+                                int64_t workspace_bytes, void* stream) {
+    using namespace scone;
+    const bool packed = x_type == SCONE_MX4;
+    const int64_t xe = mx4::elem_bytes(x_type), oe = mx4::elem_bytes(out_type);
+    if ((!packed && xe == 0) || oe == 0 || !sizes_ok(M, N, K)) return SCONE_EINVAL;
+    if (activation != SCONE_ACT_NONE && activation != SCONE_ACT_GELU) return SCONE_EINVAL;
+    const int64_t be = bias ? mx4::elem_bytes(bias_type) : 1;
+    if (be == 0) return SCONE_EINVAL;
+    constexpr int64_t kMaxLd = (int64_t)1 << 28;  // spans stay below 2^62
+    if (ld_out < N || ld_out > kMaxLd || (!packed && (ld_x < K || ld_x > kMaxLd)))
+        return SCONE_EINVAL;
+    if (M == 0 || N == 0) return SCONE_OK;
+    if (!x || !w || !out) return SCONE_EINVAL;
+    const int64_t rb = mx4::row_bytes(K);
+    if ((uintptr_t)w % 16 != 0 || (uintptr_t)x % (packed ? 16 : xe) != 0 ||
+        (uintptr_t)out % oe != 0 || (uintptr_t)residual % oe != 0 || (uintptr_t)bias % be != 0)
+        return SCONE_EINVAL;
+    // Tiles are written while others are computed: nothing that is read may lie under
+    // them, except the residual, which each element reads before it is written, where
+    // it is the output itself.
+    const int64_t out_b = ((M - 1) * ld_out + N) * oe;
+    const int64_t need = workspace_bytes_for(M, K, x_type);
+    const void* buf[5] = {x, w, bias, residual, workspace};
+    const int64_t len[5] = {packed ? M * rb : ((M - 1) * ld_x + K) * xe, N * rb, N * be, out_b,
+                            need};
+    for (int i = 0; i < 5; ++i)
+        if (buf[i] && !(i == 3 && residual == out) && overlaps(out, out_b, buf[i], len[i]))
+            return SCONE_EINVAL;
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
+            return SCONE_EINVAL;
+        for (int i = 0; i < 4; ++i)
+            if (buf[i] && overlaps(workspace, need, buf[i], len[i])) return SCONE_EINVAL;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!packed) {
+        const hipError_t e = mx4::quantize(x, x_type, M, K, ld_x, workspace, st);
+        if (e != hipSuccess) return status_of(e);
+        x = workspace;
+    }
+    const mx4::Epilogue ep{bias, residual, out, ld_out, M, N, bias_type, out_type,
+                      activation == SCONE_ACT_GELU};
+    return status_of(mx4::linear(static_cast<const uint8_t*>(x),
+                                 static_cast<const uint8_t*>(w), K, ep, st));
 }

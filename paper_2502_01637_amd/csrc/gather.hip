@@ -14,6 +14,7 @@
 // the caches leaves them to the table rows that repeat (frequent tokens).
 // The same kernel reads a host-mapped pinned table over PCIe when the rows
 // live off the accelerator.
+#include "mx4_rows.h"
 #include "row_copy.h"
 
 namespace scone {
@@ -223,4 +224,66 @@ extern "C" int scone_gather(const int32_t* fgram_ids, int64_t n_tok, const void*
     const hipError_t e = launch_gather_any(fgram_ids, n_tok, rows, n_rows, row_bytes, placement,
                                            out, err, static_cast<hipStream_t>(stream));
     return status_of(e);
+}
+
+// --------------------------------------------------------------- 4-bit rows --
+
+namespace scone {
+namespace mx4 {
+
+hipError_t quantize(const void* x, int32_t type, int64_t n_rows, int64_t cols, int64_t ld,
+                    void* rows, hipStream_t st) {
+    switch (type) {
+        case SCONE_BF16: return launch_quantize<SCONE_BF16, 4>(x, n_rows, cols, ld, rows, st);
+        case SCONE_FP16: return launch_quantize<SCONE_FP16, 4>(x, n_rows, cols, ld, rows, st);
+        default: return launch_quantize<SCONE_FP32, 2>(x, n_rows, cols, ld, rows, st);
+    }
+}
+
+}  // namespace mx4
+}  // namespace scone
+
+extern "C" int64_t scone_mx4_row_bytes(int64_t cols) {
+    return scone::mx4::cols_ok(cols) ? scone::mx4::row_bytes(cols) : -1;
+}
+
+extern "C" int scone_quantize_mx4(const void* x, int32_t x_type, int64_t n_rows, int64_t cols,
+                                  int64_t ld, void* rows, void* stream) {
+    using namespace scone;
+    const int64_t eb = mx4::elem_bytes(x_type);
+    if (eb == 0 || n_rows < 0 || !mx4::cols_ok(cols) || ld < cols) return SCONE_EINVAL;
+    if (ld > ((int64_t)1 << 56) || (n_rows > 0 && ld > ((int64_t)1 << 60) / n_rows))
+        return SCONE_EINVAL;
+    if (n_rows == 0) return SCONE_OK;
+    const int64_t rb = mx4::row_bytes(cols);
+    if (!x || !rows || (uintptr_t)x % eb != 0 || (uintptr_t)rows % 16 != 0) return SCONE_EINVAL;
+    // Rows are written while others are read.
+    if (overlaps(rows, span_bytes(n_rows, rb), x, ((n_rows - 1) * ld + cols) * eb))
+        return SCONE_EINVAL;
+    return status_of(mx4::quantize(x, x_type, n_rows, cols, ld, rows,
+                                   static_cast<hipStream_t>(stream)));
+}
+
+extern "C" int scone_gather_mx4(const int32_t* fgram_ids, int64_t n_tok, const void* rows,
+                                int64_t n_rows, int64_t cols, void* out, int32_t out_type,
+                                int32_t placement, void* stream) {
+    using namespace scone;
+    const int64_t eb = mx4::elem_bytes(out_type);
+    if (eb == 0 || n_tok < 0 || n_rows < 0 || !mx4::cols_ok(cols)) return SCONE_EINVAL;
+    if (placement != SCONE_PLACE_HBM && placement != SCONE_PLACE_HOST) return SCONE_EINVAL;
+    if (n_tok > ((int64_t)1 << 58) / cols) return SCONE_EINVAL;
+    if (!fgram_ids && n_tok > n_rows) return SCONE_EINVAL;
+    if (n_tok == 0) return SCONE_OK;
+    if (!out || (!rows && n_rows > 0)) return SCONE_EINVAL;
+    if ((uintptr_t)out % eb != 0 || (uintptr_t)rows % 16 != 0) return SCONE_EINVAL;
+    // Rows are written while other wavefronts still read their ids and rows.
+    const int64_t out_b = n_tok * cols * eb;
+    if (overlaps(out, out_b, fgram_ids, span_bytes(n_tok, 4)) ||
+        overlaps(out, out_b, rows, span_bytes(n_rows, mx4::row_bytes(cols))))
+        return SCONE_EINVAL;
+    unsigned* err = device_error_word();
+    if (!err) return SCONE_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (n_rows == 0) return status_of(launch_zero_rows(out, out_b, err, st));
+    return status_of(mx4::gather(fgram_ids, n_tok, rows, n_rows, cols, out, out_type, err, st));
 }

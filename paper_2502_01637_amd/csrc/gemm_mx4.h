@@ -8,19 +8,15 @@
 // scale byte, which the instruction applies.  Products of two codes are exact and the
 // sums are fp32.  w is the first operand, so a lane's four accumulators are four
 // consecutive n of one row m.
+#pragma once
+
 #include "gemm_bf16.h"
 #include "mx4.h"
 
 namespace scone {
-
 namespace mx4 {
-hipError_t quantize(const void* x, int32_t type, int64_t n_rows, int64_t cols, int64_t ld,
-                    void* rows, hipStream_t st);
-}  // namespace mx4
 
-namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+using gemm::f32x4;
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // What follows the sums.
@@ -64,7 +60,7 @@ __global__ __launch_bounds__(256) void k_linear(const uint8_t* __restrict__ x,
     const int64_t m0 = blk / tiles_n * 64 + (wave >> 1) * 32;
     const int64_t n0 = blk % tiles_n * 64 + (wave & 1) * 32;
     const int fr = lane & 15, q = lane >> 4;
-    const int64_t rb = mx4::row_bytes(K), g = mx4::groups(K);
+    const int64_t rb = row_bytes(K), g = groups(K);
     const uint8_t *px[2], *pw[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -104,7 +100,7 @@ __global__ __launch_bounds__(256) void k_linear(const uint8_t* __restrict__ x,
             }
 }
 
-hipError_t linear(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue& ep,
+inline hipError_t linear(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue& ep,
                   hipStream_t st) {
     const int64_t tiles_m = (ep.M + 63) / 64, tiles_n = (ep.N + 63) / 64;
     return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
@@ -112,72 +108,5 @@ hipError_t linear(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue&
     });
 }
 
-constexpr int64_t kMaxRows = (int64_t)1 << 31;
-
-bool sizes_ok(int64_t M, int64_t N, int64_t K) {
-    return M >= 0 && N >= 0 && M < kMaxRows && N < kMaxRows && mx4::cols_ok(K);
-}
-
-// 4-bit rows of x, where the call makes them.
-int64_t workspace_bytes_for(int64_t M, int64_t K, int32_t x_type) {
-    return x_type == SCONE_MX4 ? 0 : M * mx4::row_bytes(K);
-}
-
-}  // namespace
+}  // namespace mx4
 }  // namespace scone
-
-extern "C" int64_t scone_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, int32_t x_type) {
-    using namespace scone;
-    if (!sizes_ok(M, N, K) || (x_type != SCONE_MX4 && mx4::elem_bytes(x_type) == 0)) return -1;
-    return N == 0 ? 0 : workspace_bytes_for(M, K, x_type);
-}
-
-extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int64_t M, int64_t K,
-                                const void* w, int64_t N, const void* bias, int32_t bias_type,
-                                int32_t activation, const void* residual, void* out,
-                                int32_t out_type, int64_t ld_out, void* workspace,
-                                int64_t workspace_bytes, void* stream) {
-    using namespace scone;
-    const bool packed = x_type == SCONE_MX4;
-    const int64_t xe = mx4::elem_bytes(x_type), oe = mx4::elem_bytes(out_type);
-    if ((!packed && xe == 0) || oe == 0 || !sizes_ok(M, N, K)) return SCONE_EINVAL;
-    if (activation != SCONE_ACT_NONE && activation != SCONE_ACT_GELU) return SCONE_EINVAL;
-    const int64_t be = bias ? mx4::elem_bytes(bias_type) : 1;
-    if (be == 0) return SCONE_EINVAL;
-    constexpr int64_t kMaxLd = (int64_t)1 << 28;  // spans stay below 2^62
-    if (ld_out < N || ld_out > kMaxLd || (!packed && (ld_x < K || ld_x > kMaxLd)))
-        return SCONE_EINVAL;
-    if (M == 0 || N == 0) return SCONE_OK;
-    if (!x || !w || !out) return SCONE_EINVAL;
-    const int64_t rb = mx4::row_bytes(K);
-    if ((uintptr_t)w % 16 != 0 || (uintptr_t)x % (packed ? 16 : xe) != 0 ||
-        (uintptr_t)out % oe != 0 || (uintptr_t)residual % oe != 0 || (uintptr_t)bias % be != 0)
-        return SCONE_EINVAL;
-    // Tiles are written while others are computed: nothing that is read may lie under
-    // them, except the residual, which each element reads before it is written, where
-    // it is the output itself.
-    const int64_t out_b = ((M - 1) * ld_out + N) * oe;
-    const int64_t need = workspace_bytes_for(M, K, x_type);
-    const void* buf[5] = {x, w, bias, residual, workspace};
-    const int64_t len[5] = {packed ? M * rb : ((M - 1) * ld_x + K) * xe, N * rb, N * be, out_b,
-                            need};
-    for (int i = 0; i < 5; ++i)
-        if (buf[i] && !(i == 3 && residual == out) && overlaps(out, out_b, buf[i], len[i]))
-            return SCONE_EINVAL;
-    if (need > 0) {
-        if (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16 != 0)
-            return SCONE_EINVAL;
-        for (int i = 0; i < 4; ++i)
-            if (buf[i] && overlaps(workspace, need, buf[i], len[i])) return SCONE_EINVAL;
-    }
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if (!packed) {
-        const hipError_t e = mx4::quantize(x, x_type, M, K, ld_x, workspace, st);
-        if (e != hipSuccess) return status_of(e);
-        x = workspace;
-    }
-    const Epilogue ep{bias, residual, out, ld_out, M, N, bias_type, out_type,
-                      activation == SCONE_ACT_GELU};
-    return status_of(linear(static_cast<const uint8_t*>(x), static_cast<const uint8_t*>(w), K, ep,
-                            st));
-}

@@ -208,5 +208,9 @@ __device__ __forceinline__ void store8(typename Elem<kType>::type* p, int64_t n,
     }
 }
 
+// Quantise rows (the whole of scone_quantize_mx4 after its argument checks).
+hipError_t quantize(const void* x, int32_t type, int64_t n_rows, int64_t cols, int64_t ld,
+                    void* rows, hipStream_t st);
+
 }  // namespace mx4
 }  // namespace scone
