@@ -587,18 +587,13 @@ bool sizes_ok(int64_t M, int64_t N, int64_t K) {
     return M >= 0 && N >= 0 && M < kMaxRows && N < kMaxRows && mx4::cols_ok(K);
 }
 
-// 4-bit rows of x, where the call makes them.
-int64_t workspace_bytes_for(int64_t M, int64_t K, int32_t x_type) {
-    return x_type == SCONE_MX4 ? 0 : M * mx4::row_bytes(K);
-}
-
 }  // namespace
 }  // namespace scone
 
 extern "C" int64_t scone_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, int32_t x_type) {
     using namespace scone;
     if (!sizes_ok(M, N, K) || (x_type != SCONE_MX4 && mx4::elem_bytes(x_type) == 0)) return -1;
-    return N == 0 ? 0 : workspace_bytes_for(M, K, x_type);
+    return mx4::linear_workspace(M, N, K, x_type == SCONE_MX4);
 }
 
 extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int64_t M, int64_t K,
@@ -626,7 +621,7 @@ extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int
     // them, except the residual, which each element reads before it is written, where
     // it is the output itself.
     const int64_t out_b = ((M - 1) * ld_out + N) * oe;
-    const int64_t need = workspace_bytes_for(M, K, x_type);
+    const int64_t need = mx4::linear_workspace(M, N, K, packed);
     const void* buf[5] = {x, w, bias, residual, workspace};
     const int64_t len[5] = {packed ? M * rb : ((M - 1) * ld_x + K) * xe, N * rb, N * be, out_b,
                             need};
@@ -639,14 +634,9 @@ extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int
         for (int i = 0; i < 4; ++i)
             if (buf[i] && overlaps(workspace, need, buf[i], len[i])) return SCONE_EINVAL;
     }
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if (!packed) {
-        const hipError_t e = mx4::quantize(x, x_type, M, K, ld_x, workspace, st);
-        if (e != hipSuccess) return status_of(e);
-        x = workspace;
-    }
     const mx4::Epilogue ep{bias, residual, out, ld_out, M, N, bias_type, out_type,
-                      activation == SCONE_ACT_GELU};
-    return status_of(mx4::linear(static_cast<const uint8_t*>(x),
-                                 static_cast<const uint8_t*>(w), K, ep, st));
+                           activation == SCONE_ACT_GELU};
+    return status_of(mx4::linear(x, x_type, ld_x, static_cast<const uint8_t*>(w), K, ep,
+                                 static_cast<uint8_t*>(workspace),
+                                 static_cast<hipStream_t>(stream)));
 }

@@ -142,22 +142,110 @@ __device__ __forceinline__ void put4(void* p, int64_t i, const f32x4& v) {
     }
 }
 
-// s_waitcnt immediates as in gemm_bf16.h.
 using gemm::kWaitLds;
 using gemm::waitcnt_vm;
+
+// A matrix by groups, as the tiles read it: group k's codes of row r at byte
+// (k ld + r) 64, its word of scales at k ld + r, so that a slab of a tile is one run of
+// bytes.  The copies into LDS reach 37 TB/s on such runs, 13 to 16 on 64-byte pieces of
+// 4-bit rows (whose pitch is no multiple of 128) and 20 to 32 on 128-byte pieces: with
+// the rows' own layout an 8,192^3 product took 307 us, 204 of them without its copies.
+struct Slabs {
+    uint8_t* codes;
+    uint32_t* scales;
+    int64_t ld;
+};
+
+// Rows that the slabs of n rows are laid out for: a tile's scales are copied as 256
+// words from its first row on.
+__host__ __device__ inline int64_t slabs_ld(int64_t n) { return (n + 256 + 63) / 64 * 64; }
+inline int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
+inline int64_t slabs_bytes(int64_t n, int64_t K) {
+    return slabs_ld(n) * groups(K) * 64 + align256(slabs_ld(n) * groups(K) * 4);
+}
+inline Slabs slabs_at(uint8_t* at, int64_t n, int64_t K) {
+    const int64_t ld = slabs_ld(n);
+    return {at, reinterpret_cast<uint32_t*>(at + ld * groups(K) * 64), ld};
+}
+
+// 16 rows by four groups a workgroup, from 4-bit rows: a wavefront copies the codes of
+// one group, four lanes a row.
+__device__ __forceinline__ void slabs_of_rows(const uint8_t* __restrict__ rows, int64_t n, int g,
+                                              int rb, const Slabs& s, int64_t r0, int k0) {
+    const int lane = threadIdx.x & 63, k = k0 + (threadIdx.x >> 6);
+    const int64_t r = r0 + (lane >> 2);
+    if (r >= n || k >= g) return;
+    const uint8_t* row = rows + r * rb;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(row + k * 64 + (lane & 3) * 16);
+    *reinterpret_cast<u32x4*>(s.codes + (k * s.ld + r) * 64 + (lane & 3) * 16) = v;
+    if ((lane & 3) == 0)
+        s.scales[k * s.ld + r] = *reinterpret_cast<const uint32_t*>(row + 64 * (int64_t)g + k * 4);
+}
+
+// The same from rows to quantise: 16 lanes hold a group of one row, as in k_quantize,
+// a wavefront four rows and, one after another, four groups of them.
+template <int kType>
+__device__ __forceinline__ void slabs_of_elements(const typename Elem<kType>::type* __restrict__ x,
+                                                  int64_t n, int64_t cols, int64_t ld, int g,
+                                                  const Slabs& s, int64_t r0, int k0) {
+    typedef Elem<kType> E;
+    const int64_t r = r0 + (threadIdx.x >> 4);
+    const int c = threadIdx.x & 15;
+    typename E::vec v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t e = (int64_t)(k0 + u) * 128 + c * 8;
+        v[u] = load8<kType>(x + (r < n ? r * ld + e : 0), r < n ? cols - e : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        uint32_t word;
+        const uint32_t codes = quantize8<kType>(v[u], word);
+        if (r >= n || k0 + u >= g) continue;
+        const int64_t at = (k0 + u) * s.ld + r;
+        reinterpret_cast<uint32_t*>(s.codes)[at * 16 + c] = codes;
+        if (c == 0) s.scales[at] = word;
+    }
+}
+
+inline int64_t slab_blocks(int64_t n, int64_t K) {
+    return (n + 15) / 16 * ((groups(K) + 3) / 4);
+}
+
+// x's slabs (kType: its type) and then w's.
+template <int kType>
+__global__ __launch_bounds__(256) void k_slabs(const void* __restrict__ x, int64_t ld, int64_t M,
+                                               Slabs sx, const uint8_t* __restrict__ w, int64_t N,
+                                               Slabs sw, int64_t K, int64_t x_blocks,
+                                               int64_t block0) {
+    const int g = (int)groups(K), quads = (g + 3) / 4;
+    int64_t b = block_index(block0);
+    const bool of_x = b < x_blocks;
+    if (!of_x) b -= x_blocks;
+    const int64_t r0 = b / quads * 16;
+    const int k0 = (int)(b % quads) * 4;
+    if (!of_x)
+        slabs_of_rows(w, N, g, (int)row_bytes(K), sw, r0, k0);
+    else if constexpr (kType == SCONE_MX4)
+        slabs_of_rows(static_cast<const uint8_t*>(x), M, g, (int)row_bytes(K), sx, r0, k0);
+    else
+        slabs_of_elements<kType>(static_cast<const typename Elem<kType>::type*>(x), M, K, ld, g,
+                                 sx, r0, k0);
+}
 
 // A tile of 64 TM x 64 TN on four wavefronts, 32 TM x 32 TN each, in 32 x 32 x 64 scaled
 // products (measured from registers 9,550 TFLOP/s against 7,190 for 16 x 16 x 128).
 //
-// A slab is one group of 128: 64 bytes of codes per row, which go from memory
-// straight into a ring of three LDS stages.  One barrier per slab: behind it every
-// wavefront's copies of the slab have landed and its reads of the slab before are done,
-// so the stage of that one takes the copies of the slab after next.  A row's four
-// 16-byte chunks lie at slot chunk ^ ((row >> 1) & 3), so that eight lanes that read
-// one chunk of eight rows touch all banks.  Lane l of a product holds row l % 32 and
-// block l / 32 of its 64-deep half; the scale bytes of four slabs come into a lane's
-// registers as one load of its row, a group of four slabs ahead, shifted so that the
-// lane's block is byte 0 or 2 for either half.
+// A slab is one group of 128: 64 bytes of codes and a word of scales per row (Slabs),
+// which go from memory straight into a ring of three LDS stages.  A row's four 16-byte chunks
+// lie at slot chunk ^ ((row >> 2) & 3): the 16 lanes that the LDS serves at once in a
+// 16-byte read (0-3, 12-15, 20-23, 24-27, and the like) then touch every bank once.
+// Lane l of a product holds row l % 32 and block l / 32 of its 64-deep half.
+//
+// A slab is two halves, whose fragments are double buffered in registers: the reads of
+// one half run under the products of the other.  Between the halves lies the slab's one
+// barrier: behind it every wavefront holds the whole slab in registers, so its stage
+// takes the copies of the slab three further on, and the next slab has landed.
 //
 // Two such workgroups share a compute unit (128 accumulators a lane of 128 x 256), one
 // of which can store its results while the other multiplies.
@@ -166,13 +254,12 @@ using gemm::waitcnt_vm;
 // ring, and leave it by whole rows: a lane takes four consecutive n, adds the bias, and
 // rounds once behind activation and residual.
 template <int TM, int TN, int kOut, bool kResid>
-__global__ __launch_bounds__(256, 2) void k_linear_tiles(const uint8_t* __restrict__ x,
-                                                         const uint8_t* __restrict__ w, int g,
-                                                         int rb, Epilogue ep, int64_t tiles_m,
-                                                         int64_t tiles_n, int64_t block0) {
-#if defined(__HIP_DEVICE_COMPILE__)  // the host has no buffer resources
+__global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g, Epilogue ep,
+                                                         int64_t tiles_m, int64_t tiles_n,
+                                                         int64_t block0) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
-    constexpr int STAGE = (BM + BN) * 64;
+    constexpr int SX = (BM + BN) * 64, SW = SX + 1024;  // the scales behind the codes
+    constexpr int STAGE = SW + 1024;
     constexpr int PITCH = 32 * TN * 4 + 16;  // a staged row and 16 bytes against conflicts
     static_assert(4 * 32 * PITCH <= 3 * STAGE, "the staged rows take the ring's place");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[3 * STAGE];
@@ -191,64 +278,33 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(const uint8_t* __restri
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    // Rows past the end read the last row; their results are not stored.
-    const int rows_m = (int)(ep.M - m0 < BM ? ep.M - m0 : BM);
-    const int rows_n = (int)(ep.N - n0 < BN ? ep.N - n0 : BN);
-    // Buffers: the slab's place is a scalar offset, so copies take no vector arithmetic.
-    const auto px = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(x + m0 * rb), 0,
-                                                      rows_m * rb, 0x20000);
-    const auto pw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(w + n0 * rb), 0,
-                                                      rows_n * rb, 0x20000);
-    // Copies: an instruction fills 16 rows, lane l slot l % 4 of row l / 4.
-    int cx[TM], cw[TN];
-    {
-        const int chunk = ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int r = (wave * TM + i) * 16 + (lane >> 2);
-            cx[i] = (r < rows_m ? r : rows_m - 1) * rb + chunk;
-        }
-#pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const int r = (wave * TN + i) * 16 + (lane >> 2);
-            cw[i] = (r < rows_n ? r : rows_n - 1) * rb + chunk;
-        }
-    }
-    auto issue = [&](int slab) {
-        uint8_t* at = smem + slab % 3 * STAGE + wave * TM * 1024;
+    // Copies: an instruction fills 16 rows, lane l slot l % 4 of row l / 4.  Rows past
+    // the end hold anything: their results are not stored.  The scales: wavefronts 0
+    // and 2 copy x's words, 1 and 3 w's (twice, so that every wavefront counts the same
+    // copies).
+    const uint8_t* cx = x.codes + (m0 + wave * TM * 16) * 64;
+    const uint8_t* cw = w.codes + (n0 + wave * TN * 16) * 64;
+    const bool odd = wave & 1;
+    const uint32_t* cs = odd ? w.scales + n0 : x.scales + m0;
+    const int64_t scales_ld = odd ? w.ld : x.ld;
+    const uint32_t piece = (lane >> 2) * 64 + ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    auto issue = [&](int slab, int stage) {
+        uint8_t* const at = smem + stage * STAGE;
+        const uint8_t* const fx = cx + slab * x.ld * 64;
+        const uint8_t* const fw = cw + slab * w.ld * 64;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(px, (lds_ptr_t)(at + i * 1024), 16, cx[i],
-                                                     slab * 64, 0, 0);
-        at = smem + slab % 3 * STAGE + BM * 64 + wave * TN * 1024;
+            __builtin_amdgcn_global_load_lds((gemm::gbl_ptr_t)(fx + i * 1024 + piece),
+                                             (lds_ptr_t)(at + (wave * TM + i) * 1024), 16, 0, 0);
 #pragma unroll
         for (int i = 0; i < TN; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(pw, (lds_ptr_t)(at + i * 1024), 16, cw[i],
-                                                     slab * 64, 0, 0);
+            __builtin_amdgcn_global_load_lds(
+                (gemm::gbl_ptr_t)(fw + i * 1024 + piece),
+                (lds_ptr_t)(at + BM * 64 + (wave * TN + i) * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((gemm::gbl_ptr_t)(cs + slab * scales_ld + lane * 4),
+                                         (lds_ptr_t)(at + (odd ? SW : SX)), 16, 0, 0);
     };
-    const int fr = lane & 31, half = lane >> 5;
-    int sx[TM], sw[TN];  // where the lane's scale bytes are
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int r = wm * 32 * TM + i * 32 + fr;
-        sx[i] = (r < rows_m ? r : rows_m - 1) * rb + 64 * g;
-    }
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        const int r = wn * 32 * TN + i * 32 + fr;
-        sw[i] = (r < rows_n ? r : rows_n - 1) * rb + 64 * g;
-    }
-    u32x4 nx[TM], nw[TN], vx[TM], vw[TN];  // scales of the next and of this group of slabs
-    auto load_scales = [&](int slab) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-            nx[i] = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(px, sx[i], slab * 4, 0));
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-            nw[i] = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(pw, sw[i], slab * 4, 0));
-    };
+    constexpr int kCopies = TM + TN + 1;
 
     f32x16 acc[TN][TM];
 #pragma unroll
@@ -258,86 +314,110 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(const uint8_t* __restri
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    const int swz = (fr >> 1) & 3;
-    const uint8_t* fx = smem + (wm * 32 * TM + fr) * 64;
-    const uint8_t* fw = smem + BM * 64 + (wn * 32 * TN + fr) * 64;
-    constexpr int kCopies = TM + TN;
-
-    // Slab k, the j-th of its group.  kWhole: slabs k + 1 and k + 2 and the next group's
-    // scales exist; otherwise that is looked up.
-    auto step = [&](int k, auto j_c, bool more, auto whole_c) {
-        constexpr int j = decltype(j_c)::value;
-        constexpr bool kWhole = decltype(whole_c)::value;
-        // What may be outstanding behind slab k: the copies of slab k + 1 and, until
-        // the last slab of the group, the next scales.
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(kWaitLds);
-        if (kWhole || (k + 1 < g && more))
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(j == 1 || j == 2 ? 2 * kCopies : kCopies));
-        else if (k + 1 < g)
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(kCopies));
-        else
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if (j == 0) {
+    const int fr = lane & 31, half = lane >> 5;
+    const int swz = (fr >> 2) & 3;
+    const int slots[2] = {(half ^ swz) * 16, ((2 + half) ^ swz) * 16};
+    const uint8_t* const fx = smem + (wm * 32 * TM + fr) * 64;
+    const uint8_t* const fw = smem + BM * 64 + (wn * 32 * TN + fr) * 64;
+    const uint8_t* const gx = smem + SX + (wm * 32 * TM + fr) * 4;
+    const uint8_t* const gw = smem + SW + (wn * 32 * TN + fr) * 4;
+    u32x4 a0[TN], b0[TM], a1[TN], b1[TM];    // fragments of halves 0 and 1
+    uint32_t va[TN], vb[TM], na[TN], nb[TM];  // scales of this slab and the next
+    auto read = [&](int stage, int h, u32x4 (&a)[TN], u32x4 (&b)[TM]) {
+        const int at = stage * STAGE + slots[h];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) vx[i] = nx[i] >> (8 * half);
+        for (int i = 0; i < TN; ++i) a[i] = *reinterpret_cast<const u32x4*>(fw + at + i * 2048);
 #pragma unroll
-            for (int i = 0; i < TN; ++i) vw[i] = nw[i] >> (8 * half);
-        }
-        if (kWhole || k + 2 < g) issue(k + 2);
-        if (j == 0 && (kWhole || more)) {
-            __builtin_amdgcn_sched_barrier(0);  // the waits count on this order
-            load_scales(k + 4);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        const int at = k % 3 * STAGE;
+        for (int i = 0; i < TM; ++i) b[i] = *reinterpret_cast<const u32x4*>(fx + at + i * 2048);
+    };
+    auto read_scales = [&](int stage) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int slot = at + ((h * 2 + half) ^ swz) * 16;
-            i32x8 a[TN], b[TM];
+        for (int i = 0; i < TN; ++i)
+            na[i] = *reinterpret_cast<const uint32_t*>(gw + stage * STAGE + i * 128);
 #pragma unroll
-            for (int i = 0; i < TN; ++i) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(fw + slot + i * 2048);
-                a[i] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+        for (int i = 0; i < TM; ++i)
+            nb[i] = *reinterpret_cast<const uint32_t*>(gx + stage * STAGE + i * 128);
+    };
+    auto take_scales = [&]() {  // the lane's blocks become bytes 0 and 2
+#pragma unroll
+        for (int i = 0; i < TN; ++i) va[i] = na[i] >> (8 * half);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) vb[i] = nb[i] >> (8 * half);
+    };
+    auto multiply = [&](auto h_c, const u32x4 (&a)[TN], const u32x4 (&b)[TM]) {
+        constexpr int kByte = decltype(h_c)::value * 2;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            const i32x8 av = {(int)a[i][0], (int)a[i][1], (int)a[i][2], (int)a[i][3], 0, 0, 0, 0};
+#pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                const i32x8 bv = {(int)b[m][0], (int)b[m][1], (int)b[m][2], (int)b[m][3], 0, 0, 0, 0};
+                acc[i][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    av, bv, acc[i][m], 4, 4, kByte, (int)va[i], kByte, (int)vb[m]);
             }
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(fx + slot + i * 2048);
-                b[i] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < TN; ++i)
-#pragma unroll
-                for (int m = 0; m < TM; ++m) {
-                    const int sa = (int)vw[i][j], sb = (int)vx[m][j];
-                    acc[i][m] = h == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                                             a[i], b[m], acc[i][m], 4, 4, 0, sa, 0, sb)
-                                       : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                                             a[i], b[m], acc[i][m], 4, 4, 2, sa, 2, sb);
-                }
         }
     };
     using std::integral_constant;
-    load_scales(0);
-    issue(0);
-    if (g > 1) issue(1);
-    int k0 = 0;
-    for (; k0 + 5 < g; k0 += 4) {
-        step(k0, integral_constant<int, 0>{}, true, std::true_type{});
-        step(k0 + 1, integral_constant<int, 1>{}, true, std::true_type{});
-        step(k0 + 2, integral_constant<int, 2>{}, true, std::true_type{});
-        step(k0 + 3, integral_constant<int, 3>{}, true, std::true_type{});
+    constexpr int kMfma = 0x008, kVmemRead = 0x020, kDsRead = 0x100;
+    // Slab k in stage `st`, its first half's fragments and scales in registers.
+    // kMore: how many of the slabs behind it exist, up to three.
+    auto step = [&](int k, int st, auto more_c) {
+        constexpr int kMore = decltype(more_c)::value;
+        const int next = st == 2 ? 0 : st + 1;
+        take_scales();
+        read(st, 1, a1, b1);
+        multiply(integral_constant<int, 0>{}, a0, b0);
+#pragma unroll
+        for (int i = 0; i < TM + TN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kMore >= 1) {
+            __builtin_amdgcn_s_waitcnt(kWaitLds);
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(kMore >= 2 ? kCopies : 0));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kMore >= 3) issue(k + 3, st);
+            read_scales(next);
+            read(next, 0, a0, b0);
+        }
+        multiply(integral_constant<int, 1>{}, a1, b1);
+        if constexpr (kMore >= 1) {
+#pragma unroll
+            for (int i = 0; i < TN * TM; ++i) {
+                if constexpr (kMore >= 3) __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    issue(0, 0);
+    if (g > 1) issue(1, 1);
+    if (g > 2) issue(2, 2);
+    if (g > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kCopies));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    read_scales(0);
+    read(0, 0, a0, b0);
+    int k = 0, st = 0;
+    for (; k + 3 < g; ++k) {
+        step(k, st, integral_constant<int, 3>{});
+        st = st == 2 ? 0 : st + 1;
     }
-    for (; k0 < g; k0 += 4) {
-        const bool more = k0 + 4 < g;
-        step(k0, integral_constant<int, 0>{}, more, std::false_type{});
-        if (k0 + 1 < g) step(k0 + 1, integral_constant<int, 1>{}, more, std::false_type{});
-        if (k0 + 2 < g) step(k0 + 2, integral_constant<int, 2>{}, more, std::false_type{});
-        if (k0 + 3 < g) step(k0 + 3, integral_constant<int, 3>{}, more, std::false_type{});
+    if (k + 2 < g) {
+        step(k++, st, integral_constant<int, 2>{});
+        st = st == 2 ? 0 : st + 1;
     }
+    if (k + 1 < g) {
+        step(k++, st, integral_constant<int, 1>{});
+        st = st == 2 ? 0 : st + 1;
+    }
+    step(k, st, integral_constant<int, 0>{});
 
     // acc[i][m][r] is out[row m * 32 + lane % 32, n i * 32 + 8 (r / 4) + 4 (lane / 32) + r % 4].
     __builtin_amdgcn_sched_barrier(0);
@@ -406,22 +486,21 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(const uint8_t* __restri
             }
         }
     }
-#endif
 }
 
 template <int TM, int TN, int kOut, bool kResid>
-inline hipError_t launch_tiles(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue& ep,
+inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
                                hipStream_t st) {
     const int64_t tiles_m = (ep.M + 64 * TM - 1) / (64 * TM);
     const int64_t tiles_n = (ep.N + 64 * TN - 1) / (64 * TN);
     return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
-        hipLaunchKernelGGL((k_linear_tiles<TM, TN, kOut, kResid>), grid, dim3(256), 0, st, x, w,
-                           (int)groups(K), (int)row_bytes(K), ep, tiles_m, tiles_n, b0);
+        hipLaunchKernelGGL((k_linear_tiles<TM, TN, kOut, kResid>), grid, dim3(256), 0, st, x,
+                           w, (int)groups(K), ep, tiles_m, tiles_n, b0);
     });
 }
 
 template <int TM, int TN>
-inline hipError_t launch_tiles(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue& ep,
+inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
                                hipStream_t st) {
     const bool r = ep.residual != nullptr;
     switch (ep.out_type) {
@@ -437,16 +516,53 @@ inline hipError_t launch_tiles(const uint8_t* x, const uint8_t* w, int64_t K, co
     }
 }
 
-inline hipError_t linear(const uint8_t* x, const uint8_t* w, int64_t K, const Epilogue& ep,
-                         hipStream_t st) {
-    if (ep.M > 64) {
-        const int64_t big = ((ep.M + 127) / 128) * ((ep.N + 255) / 256);
-        return big >= 256 ? launch_tiles<2, 4>(x, w, K, ep, st) : launch_tiles<1, 2>(x, w, K, ep, st);
-    }
-    const int64_t tiles_m = (ep.M + 63) / 64, tiles_n = (ep.N + 63) / 64;
-    return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
-        hipLaunchKernelGGL(k_linear, grid, dim3(256), 0, st, x, w, K, ep, tiles_n, b0);
+// Whether a product takes the tiles.
+inline bool tiled(int64_t M) { return M > 64; }
+
+// Scratch of a linear map: the slabs of x and w, or x in 4 bits where the call makes it.
+inline int64_t linear_workspace(int64_t M, int64_t N, int64_t K, bool packed) {
+    if (M == 0 || N == 0) return 0;
+    if (tiled(M)) return slabs_bytes(M, K) + slabs_bytes(N, K);
+    return packed ? 0 : M * row_bytes(K);
+}
+
+template <int kType>
+inline hipError_t launch_slabs(const void* x, int64_t ld, int64_t M, const Slabs& sx,
+                               const uint8_t* w, int64_t N, const Slabs& sw, int64_t K,
+                               hipStream_t st) {
+    const int64_t bx = slab_blocks(M, K);
+    return launch_blocks(bx + slab_blocks(N, K), 256, [&](int64_t b0, dim3 grid) {
+        hipLaunchKernelGGL(k_slabs<kType>, grid, dim3(256), 0, st, x, ld, M, sx, w, N, sw, K, bx,
+                           b0);
     });
+}
+
+// x: 4-bit rows, or (type not SCONE_MX4) rows to quantise.
+inline hipError_t linear(const void* x, int32_t type, int64_t ld, const uint8_t* w, int64_t K,
+                         const Epilogue& ep, uint8_t* ws, hipStream_t st) {
+    if (!tiled(ep.M)) {
+        const uint8_t* rows = static_cast<const uint8_t*>(x);
+        if (type != SCONE_MX4) {
+            const hipError_t e = quantize(x, type, ep.M, K, ld, ws, st);
+            if (e != hipSuccess) return e;
+            rows = ws;
+        }
+        const int64_t tiles_m = (ep.M + 63) / 64, tiles_n = (ep.N + 63) / 64;
+        return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
+            hipLaunchKernelGGL(k_linear, grid, dim3(256), 0, st, rows, w, K, ep, tiles_n, b0);
+        });
+    }
+    const Slabs sx = slabs_at(ws, ep.M, K), sw = slabs_at(ws + slabs_bytes(ep.M, K), ep.N, K);
+    hipError_t e;
+    switch (type) {
+        case SCONE_BF16: e = launch_slabs<SCONE_BF16>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
+        case SCONE_FP16: e = launch_slabs<SCONE_FP16>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
+        case SCONE_FP32: e = launch_slabs<SCONE_FP32>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
+        default: e = launch_slabs<SCONE_MX4>(x, ld, ep.M, sx, w, ep.N, sw, K, st);
+    }
+    if (e != hipSuccess) return e;
+    const int64_t big = ((ep.M + 127) / 128) * ((ep.N + 255) / 256);
+    return big >= 256 ? launch_tiles<2, 4>(sx, sw, K, ep, st) : launch_tiles<1, 2>(sx, sw, K, ep, st);
 }
 
 }  // namespace mx4

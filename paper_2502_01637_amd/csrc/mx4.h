@@ -158,6 +158,25 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t field) {
     return field == 255 ? 255u : field < 2 ? 0u : field - 2;
 }
 
+// Codes of eight elements, 16 lanes in a row holding a group of 128: each block of 32 is
+// four lanes, whose largest magnitudes are joined by two exchanges; the group's four
+// scale bytes are joined to a word the same way.
+template <int kType>
+__device__ __forceinline__ uint32_t quantize8(const typename Elem<kType>::vec& v,
+                                              uint32_t& word) {
+    typedef Elem<kType> E;
+    uint32_t top = E::top(v);
+    uint32_t o = __shfl_xor(top, 1);
+    top = top > o ? top : o;
+    o = __shfl_xor(top, 2);
+    top = top > o ? top : o;
+    const uint32_t s = scale_byte(E::field(top));
+    word = s << (8 * ((threadIdx.x >> 2) & 3));
+    word |= __shfl_xor(word, 4);
+    word |= __shfl_xor(word, 8);
+    return s == 255 ? 0u : E::quantize(v, scale_of(s));
+}
+
 // Eight elements from address p, of which the first n are there (n < 8: one by one).
 template <int kType>
 __device__ __forceinline__ typename Elem<kType>::vec load8(

@@ -14,10 +14,8 @@ namespace mx4 {
 
 constexpr int kThreads = 256;
 
-// Quantisation: each block of 32 is four lanes, whose largest magnitudes are joined
-// by two exchanges; sixteen lanes hold a group of 128, whose four scale bytes are
-// joined to a word the same way.  A row's 16 g pieces are a multiple of 16, so blocks
-// and groups lie inside one row and one aligned run of lanes.
+// Quantisation.  A row's 16 g pieces are a multiple of 16, so a group lies inside one
+// row and one aligned run of 16 lanes, as quantize8 takes it.
 template <int kType, int U>
 __global__ __launch_bounds__(kThreads) void k_quantize(
     const typename Elem<kType>::type* __restrict__ x, int64_t n_rows, int64_t cols,
@@ -41,16 +39,8 @@ __global__ __launch_bounds__(kThreads) void k_quantize(
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        uint32_t top = E::top(v[u]);
-        uint32_t o = __shfl_xor(top, 1);
-        top = top > o ? top : o;
-        o = __shfl_xor(top, 2);
-        top = top > o ? top : o;
-        const uint32_t s = scale_byte(E::field(top));
-        const uint32_t codes = s == 255 ? 0u : E::quantize(v[u], scale_of(s));
-        uint32_t word = s << (8 * ((threadIdx.x >> 2) & 3));
-        word |= __shfl_xor(word, 4);
-        word |= __shfl_xor(word, 8);
+        uint32_t word;
+        const uint32_t codes = quantize8<kType>(v[u], word);
         if (r[u] >= n_rows) continue;
         uint8_t* row = rows + r[u] * row_bytes;
         reinterpret_cast<uint32_t*>(row)[c[u]] = codes;
