@@ -103,43 +103,53 @@ __global__ __launch_bounds__(256) void k_linear(const uint8_t* __restrict__ x,
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 using gemm::lds_ptr_t;
 
-// Four values to or from consecutive elements of a type.
+// 16 bytes of a type as floats: four of fp32, eight of the others.
 template <int kType>
-__device__ __forceinline__ f32x4 load4(const void* p, int64_t i) {
-    if constexpr (kType == SCONE_FP32) {
-        typedef float f32x4_elem __attribute__((ext_vector_type(4), aligned(4)));
-        return *reinterpret_cast<const f32x4_elem*>(static_cast<const float*>(p) + i);
-    } else {
-        typedef uint32_t u32x2_elem __attribute__((ext_vector_type(2), aligned(2)));
-        const u32x2 v = *reinterpret_cast<const u32x2_elem*>(static_cast<const uint16_t*>(p) + i);
-        f32x4 f;
+constexpr int kPer16 = kType == SCONE_FP32 ? 4 : 8;
+
+template <int kType>
+__device__ __forceinline__ void widen(const u32x4& v, float (&f)[kPer16<kType>]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t h = (v[k / 2] >> (16 * (k & 1))) & 0xFFFFu;
-            f[k] = kType == SCONE_BF16 ? gemm::bf16_to_f32(h)
-                                       : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
-        }
-        return f;
+    for (int i = 0; i < kPer16<kType>; ++i) {
+        if constexpr (kType == SCONE_FP32) f[i] = __uint_as_float(v[i]);
+        else if constexpr (kType == SCONE_BF16)
+            f[i] = __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
+        else f[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i / 2] >> (16 * (i & 1))));
     }
 }
 
 template <int kType>
-__device__ __forceinline__ void put4(void* p, int64_t i, const f32x4& v) {
-    if constexpr (kType == SCONE_FP32) {
-        typedef float f32x4_elem __attribute__((ext_vector_type(4), aligned(4)));
-        __builtin_nontemporal_store(v, reinterpret_cast<f32x4_elem*>(static_cast<float*>(p) + i));
-    } else {
-        typedef uint32_t u32x2_elem __attribute__((ext_vector_type(2), aligned(2)));
-        u32x2 o;
-        if constexpr (kType == SCONE_BF16) {
-            o.x = gemm::pack_bf16x2(v[0], v[1]);
-            o.y = gemm::pack_bf16x2(v[2], v[3]);
-        } else {
-            o.x = __builtin_bit_cast(uint32_t, f16x2{(_Float16)v[0], (_Float16)v[1]});
-            o.y = __builtin_bit_cast(uint32_t, f16x2{(_Float16)v[2], (_Float16)v[3]});
-        }
-        __builtin_nontemporal_store(o, reinterpret_cast<u32x2_elem*>(static_cast<uint16_t*>(p) + i));
+__device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (kType == SCONE_FP32) v[i] = __float_as_uint(f[i]);
+        else if constexpr (kType == SCONE_BF16) v[i] = gemm::pack_bf16x2(f[2 * i], f[2 * i + 1]);
+        else v[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)f[2 * i], (_Float16)f[2 * i + 1]});
     }
+    return v;
+}
+
+// GELU for results that are rounded to 16 bits: gemm::gelu_erf's form with a polynomial
+// of degree 5 on [0, 5.5] (closest in the largest relative error, weighted down beyond
+// 3).  Within 4.4e-5 of the value down to x = -3 and 6.1e-6 of it anywhere, where the
+// rounding is 2^-9 (bf16) or 2^-11 (fp16): a product whose results were GELUs of
+// degree 9 spent as long on them as on its sums.
+__device__ __forceinline__ float gelu_16(float x) {
+    const float z = __builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.0f, 5.5f);
+    float p = -3.74266548e-04f;
+    p = p * z + 6.33217741e-03f;
+    p = p * z - 4.98651324e-02f;
+    p = p * z - 4.62025925e-01f;
+    p = p * z - 1.15009108f;
+    p = p * z - 1.00006211f;
+    const float pos = __builtin_fmaf(0.5f, __builtin_fabsf(x), 0.5f * x);
+    return pos - z * __builtin_amdgcn_exp2f(p);
+}
+
+template <int kOut>
+__device__ __forceinline__ float gelu_for(float x) {
+    return kOut == SCONE_FP32 ? gemm::gelu_erf(x) : gelu_16(x);
 }
 
 using gemm::kWaitLds;
@@ -154,18 +164,19 @@ struct Slabs {
     uint8_t* codes;
     uint32_t* scales;
     int64_t ld;
+    float* bias;  // w's: what is added to row r's products
 };
 
-// Rows that the slabs of n rows are laid out for: a tile's scales are copied as 256
-// words from its first row on.
-__host__ __device__ inline int64_t slabs_ld(int64_t n) { return (n + 256 + 63) / 64 * 64; }
-inline int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
-inline int64_t slabs_bytes(int64_t n, int64_t K) {
-    return slabs_ld(n) * groups(K) * 64 + align256(slabs_ld(n) * groups(K) * 4);
-}
+// Rows are laid out up to a multiple of the largest tile, and 64 more, which keep the
+// groups of a row off powers of two; what lies past the last row is never written, and
+// only feeds results that are never stored.
+inline int64_t slabs_ld(int64_t n) { return (n + 255) / 256 * 256 + 64; }
+inline int64_t slabs_bytes(int64_t n, int64_t K) { return slabs_ld(n) * (groups(K) * 68 + 4); }
 inline Slabs slabs_at(uint8_t* at, int64_t n, int64_t K) {
     const int64_t ld = slabs_ld(n);
-    return {at, reinterpret_cast<uint32_t*>(at + ld * groups(K) * 64), ld};
+    uint8_t* const words = at + ld * groups(K) * 64;
+    return {at, reinterpret_cast<uint32_t*>(words), ld,
+            reinterpret_cast<float*>(words + ld * groups(K) * 4)};
 }
 
 // 16 rows by four groups a workgroup, from 4-bit rows: a wavefront copies the codes of
@@ -212,11 +223,12 @@ inline int64_t slab_blocks(int64_t n, int64_t K) {
     return (n + 15) / 16 * ((groups(K) + 3) / 4);
 }
 
-// x's slabs (kType: its type) and then w's.
+// x's slabs (kType: its type) and then w's, with the biases as floats.
 template <int kType>
 __global__ __launch_bounds__(256) void k_slabs(const void* __restrict__ x, int64_t ld, int64_t M,
                                                Slabs sx, const uint8_t* __restrict__ w, int64_t N,
-                                               Slabs sw, int64_t K, int64_t x_blocks,
+                                               Slabs sw, const void* __restrict__ bias,
+                                               int32_t bias_type, int64_t K, int64_t x_blocks,
                                                int64_t block0) {
     const int g = (int)groups(K), quads = (g + 3) / 4;
     int64_t b = block_index(block0);
@@ -224,13 +236,23 @@ __global__ __launch_bounds__(256) void k_slabs(const void* __restrict__ x, int64
     if (!of_x) b -= x_blocks;
     const int64_t r0 = b / quads * 16;
     const int k0 = (int)(b % quads) * 4;
-    if (!of_x)
+    if (!of_x) {
+        const int64_t r = r0 + threadIdx.x;
+        if (k0 == 0 && threadIdx.x < 16 && r < N)
+            sw.bias[r] = bias ? load_elem(bias, bias_type, r) : 0.f;
         slabs_of_rows(w, N, g, (int)row_bytes(K), sw, r0, k0);
-    else if constexpr (kType == SCONE_MX4)
+    } else if constexpr (kType == SCONE_MX4)
         slabs_of_rows(static_cast<const uint8_t*>(x), M, g, (int)row_bytes(K), sx, r0, k0);
     else
         slabs_of_elements<kType>(static_cast<const typename Elem<kType>::type*>(x), M, K, ld, g,
                                  sx, r0, k0);
+}
+
+// A stage of the ring, and the workgroups of a compute unit that its 160 KiB hold.
+constexpr int stage_bytes(int tm, int tn) { return 64 * (tm + tn) * 68; }
+constexpr int workgroups(int tm, int tn) {
+    const int n = (160 << 10) / (3 * stage_bytes(tm, tn));
+    return n < 4 ? n : 4;
 }
 
 // A tile of 64 TM x 64 TN on four wavefronts, 32 TM x 32 TN each, in 32 x 32 x 64 scaled
@@ -254,12 +276,12 @@ __global__ __launch_bounds__(256) void k_slabs(const void* __restrict__ x, int64
 // ring, and leave it by whole rows: a lane takes four consecutive n, adds the bias, and
 // rounds once behind activation and residual.
 template <int TM, int TN, int kOut, bool kResid>
-__global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g, Epilogue ep,
-                                                         int64_t tiles_m, int64_t tiles_n,
+__global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(Slabs x, Slabs w, int g, Epilogue ep,
+                                                         uint32_t tiles_m, uint32_t tiles_n,
                                                          int64_t block0) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
-    constexpr int SX = (BM + BN) * 64, SW = SX + 1024;  // the scales behind the codes
-    constexpr int STAGE = SW + 1024;
+    constexpr int SX = (BM + BN) * 64;  // x's and w's scales behind the codes
+    constexpr int STAGE = stage_bytes(TM, TN);
     constexpr int PITCH = 32 * TN * 4 + 16;  // a staged row and 16 bytes against conflicts
     static_assert(4 * 32 * PITCH <= 3 * STAGE, "the staged rows take the ring's place");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[3 * STAGE];
@@ -267,26 +289,22 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g
     int64_t m0, n0;
     {
         // As gemm::tile_at: each XCD a run of tiles, eight rows of tiles a group.
-        const int64_t nb = tiles_m * tiles_n, b = block_index(block0), per = nb / 8;
-        const int64_t t = b < per * 8 ? (b % 8) * per + b / 8 : b;
-        const int64_t group = t / (8 * tiles_n), first = group * 8;
-        const int64_t gm = tiles_m - first < 8 ? tiles_m - first : 8;
-        const int64_t tr = t - group * 8 * tiles_n;
-        m0 = (first + tr % gm) * BM;
-        n0 = tr / gm * BN;
+        const uint32_t nb = tiles_m * tiles_n, b = (uint32_t)block_index(block0), per = nb / 8;
+        const uint32_t t = b < per * 8 ? (b % 8) * per + b / 8 : b;
+        const uint32_t group = t / (8 * tiles_n), first = group * 8;
+        const uint32_t gm = tiles_m - first < 8 ? tiles_m - first : 8;
+        const uint32_t tr = t - group * 8 * tiles_n, tn = tr / gm;
+        m0 = (int64_t)(first + tr - tn * gm) * BM;
+        n0 = (int64_t)tn * BN;
     }
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    // Copies: an instruction fills 16 rows, lane l slot l % 4 of row l / 4.  Rows past
-    // the end hold anything: their results are not stored.  The scales: wavefronts 0
-    // and 2 copy x's words, 1 and 3 w's (twice, so that every wavefront counts the same
-    // copies).
-    const uint8_t* cx = x.codes + (m0 + wave * TM * 16) * 64;
-    const uint8_t* cw = w.codes + (n0 + wave * TN * 16) * 64;
-    const bool odd = wave & 1;
-    const uint32_t* cs = odd ? w.scales + n0 : x.scales + m0;
-    const int64_t scales_ld = odd ? w.ld : x.ld;
+    // Copies: an instruction fills 16 rows, lane l slot l % 4 of row l / 4; of the scales
+    // 64 words.  Every wavefront issues as many (some words twice), as the waits count.
+    constexpr int T = TM + TN, kScaleCopies = (T + 3) / 4, kCopies = T + kScaleCopies;
+    const uint8_t* const cx = x.codes + (m0 + wave * TM * 16) * 64;
+    const uint8_t* const cw = w.codes + (n0 + wave * TN * 16) * 64;
     const uint32_t piece = (lane >> 2) * 64 + ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
     auto issue = [&](int slab, int stage) {
         uint8_t* const at = smem + stage * STAGE;
@@ -301,26 +319,44 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g
             __builtin_amdgcn_global_load_lds(
                 (gemm::gbl_ptr_t)(fw + i * 1024 + piece),
                 (lds_ptr_t)(at + BM * 64 + (wave * TN + i) * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gemm::gbl_ptr_t)(cs + slab * scales_ld + lane * 4),
-                                         (lds_ptr_t)(at + (odd ? SW : SX)), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kScaleCopies; ++i) {
+            const int q = (wave + 4 * i) % T;
+            const uint32_t* const fs = q < TM ? x.scales + slab * x.ld + m0 + q * 64
+                                              : w.scales + slab * w.ld + n0 + (q - TM) * 64;
+            __builtin_amdgcn_global_load_lds((gemm::gbl_ptr_t)(fs + lane),
+                                             (lds_ptr_t)(at + SX + q * 256), 4, 0, 0);
+        }
     };
-    constexpr int kCopies = TM + TN + 1;
 
+    // The sums begin with the biases; acc[i][m][r] is out[row m * 32 + lane % 32,
+    // n i * 32 + 8 (r / 4) + 4 (lane / 32) + r % 4] of the wavefront's part.
+    const int fr = lane & 31, half = lane >> 5;
+    f32x4 bias[TN][4];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            bias[i][q] = *reinterpret_cast<const f32x4*>(w.bias + n0 + (wn * TN + i) * 32 + q * 8 +
+                                                         half * 4);
+    // Three slabs in flight (the last again where there are fewer).
+    issue(0, 0);
+    issue(g > 1 ? 1 : 0, 1);
+    issue(g > 2 ? 2 : g - 1, 2);
     f32x16 acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int j = 0; j < TM; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = bias[i][r / 4][r % 4];
 
-    const int fr = lane & 31, half = lane >> 5;
     const int swz = (fr >> 2) & 3;
     const int slots[2] = {(half ^ swz) * 16, ((2 + half) ^ swz) * 16};
     const uint8_t* const fx = smem + (wm * 32 * TM + fr) * 64;
     const uint8_t* const fw = smem + BM * 64 + (wn * 32 * TN + fr) * 64;
     const uint8_t* const gx = smem + SX + (wm * 32 * TM + fr) * 4;
-    const uint8_t* const gw = smem + SW + (wn * 32 * TN + fr) * 4;
+    const uint8_t* const gw = smem + SX + (BM + wn * 32 * TN + fr) * 4;
     u32x4 a0[TN], b0[TM], a1[TN], b1[TM];    // fragments of halves 0 and 1
     uint32_t va[TN], vb[TM], na[TN], nb[TM];  // scales of this slab and the next
     auto read = [&](int stage, int h, u32x4 (&a)[TN], u32x4 (&b)[TM]) {
@@ -394,11 +430,7 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    issue(0, 0);
-    if (g > 1) issue(1, 1);
-    if (g > 2) issue(2, 2);
-    if (g > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kCopies));
-    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * kCopies));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -419,69 +451,94 @@ __global__ __launch_bounds__(256, 2) void k_linear_tiles(Slabs x, Slabs w, int g
     }
     step(k, st, integral_constant<int, 0>{});
 
-    // acc[i][m][r] is out[row m * 32 + lane % 32, n i * 32 + 8 (r / 4) + 4 (lane / 32) + r % 4].
+    // With a single slab the copies of the other two stages may still be on their way
+    // to where the results are staged; otherwise nothing is outstanding.
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_sched_barrier(0);
+    // On the way out an instruction takes RPI rows, LPR lanes a row, V n (16 bytes) a lane;
+    // NB batches of NI of them, whose residuals are loaded a batch ahead.
+    constexpr int V = kPer16<kOut>, LPR = 32 * TN / V, RPI = 64 / LPR;
+    constexpr int NI = 32 / RPI < 8 ? 32 / RPI : 8, NB = TM * (32 / RPI / NI);
+    typedef uint32_t u32x4_out __attribute__((ext_vector_type(4), aligned(2)));
+    constexpr int kSize = 16 / V;
+    const int er = lane / LPR, ec = lane % LPR * V;
+    const int64_t row0 = m0 + wm * TM * 32 + er, n = n0 + wn * 32 * TN + ec;
+    const int64_t at0 = row0 * ep.ld + n;
+    const bool inside = m0 + BM <= ep.M && n0 + BN <= ep.N;
+    const int rows = (int)(ep.M - row0 < 32 * TM ? ep.M - row0 : 32 * TM);  // from row0 on
+    const int left = (int)(ep.N - n < V ? ep.N - n : V);                     // and columns
+    u32x4 res[2][kResid ? NI : 1];
+    auto load_residuals = [&](int batch, u32x4 (&v)[kResid ? NI : 1]) {
+        if constexpr (kResid) {
+            const uint8_t* p = static_cast<const uint8_t*>(ep.residual) +
+                               (at0 + (int64_t)batch * NI * RPI * ep.ld) * kSize;
+#pragma unroll
+            for (int u = 0; u < NI; ++u, p += RPI * ep.ld * kSize) {
+                if (inside) {
+                    v[u] = *reinterpret_cast<const u32x4_out*>(p);
+                } else {
+                    v[u] = u32x4{0, 0, 0, 0};
+                    if ((batch * NI + u) * RPI >= rows) continue;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        if (e >= left) continue;
+                        if constexpr (kSize == 4) v[u][e] = reinterpret_cast<const uint32_t*>(p)[e];
+                        else v[u][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+                    }
+                }
+            }
+        }
+    };
+    load_residuals(0, res[0]);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(kWaitLds);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    uint8_t* part = smem + wave * 32 * PITCH;
-    constexpr int LPR = 8 * TN;     // lanes a row, four n each
-    constexpr int RPI = 64 / LPR;   // rows an instruction
-    constexpr int kBatch = 4;       // instructions whose residuals are in flight together
-    const int er = lane / LPR, ec = lane % LPR * 4;
-    const int64_t n = n0 + wn * 32 * TN + ec;
-    const int left = (int)(ep.N - n < 4 ? (ep.N - n < 0 ? 0 : ep.N - n) : 4);
-    f32x4 bias = {0.f, 0.f, 0.f, 0.f};
-    if (ep.bias)
+    uint8_t* const part = smem + wave * 32 * PITCH;
+    uint8_t* po = static_cast<uint8_t*>(ep.out) + at0 * kSize;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) bias[e] = load_elem(ep.bias, ep.bias_type, n + e);
+    for (int batch = 0; batch < NB; ++batch) {
+        constexpr int kPerRowSet = NB / TM;  // batches per 32 rows
+        if (batch % kPerRowSet == 0) {
+            const int m = batch / kPerRowSet;
 #pragma unroll
-    for (int m = 0; m < TM; ++m) {
+            for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4*>(part + fr * PITCH + (i * 32 + q * 8 + half * 4) * 4) =
+                        f32x4{acc[i][m][q * 4], acc[i][m][q * 4 + 1], acc[i][m][q * 4 + 2],
+                              acc[i][m][q * 4 + 3]};
+        }
+        if (batch + 1 < NB) load_residuals(batch + 1, res[(batch + 1) & 1]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4*>(part + fr * PITCH + (i * 32 + q * 8 + half * 4) * 4) =
-                    f32x4{acc[i][m][q * 4], acc[i][m][q * 4 + 1], acc[i][m][q * 4 + 2],
-                          acc[i][m][q * 4 + 3]};
-        const int64_t row0 = m0 + (wm * TM + m) * 32 + er;
+        for (int u = 0; u < NI; ++u, po += RPI * ep.ld * kSize) {
+            const int r = (batch % kPerRowSet * NI + u) * RPI + er;
+            float v[V];
 #pragma unroll
-        for (int it = 0; it < 32 / RPI; it += kBatch) {
-            f32x4 res[kBatch];
-            if constexpr (kResid) {
+            for (int e = 0; e < V; e += 4) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(part + r * PITCH + (ec + e) * 4);
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const int64_t row = row0 + (it + u) * RPI;
-                    res[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    if (row < ep.M) {
-                        if (left == 4) res[u] = load4<kOut>(ep.residual, row * ep.ld + n);
-                        else
-#pragma unroll
-                            for (int e = 0; e < 3; ++e)
-                                if (e < left) res[u][e] = load_elem(ep.residual, kOut, row * ep.ld + n + e);
-                    }
-                }
+                for (int k = 0; k < 4; ++k) v[e + k] = s[k];
             }
+            if (ep.gelu)
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int64_t row = row0 + (it + u) * RPI;
-                f32x4 v = *reinterpret_cast<const f32x4*>(part + ((it + u) * RPI + er) * PITCH + ec * 4);
+                for (int e = 0; e < V; ++e) v[e] = gelu_for<kOut>(v[e]);
+            if constexpr (kResid) {
+                float f[V];
+                widen<kOut>(res[batch & 1][u], f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += bias[e];
-                if (ep.gelu)
+                for (int e = 0; e < V; ++e) v[e] += f[e];
+            }
+            const u32x4 o = narrow<kOut>(v);
+            if (inside) {
+                __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(po));
+            } else if ((batch * NI + u) * RPI < rows) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = gemm::gelu_erf(v[e]);
-                if constexpr (kResid)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += res[u][e];
-                if (row < ep.M) {
-                    if (left == 4) put4<kOut>(ep.out, row * ep.ld + n, v);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (e < left) store_elem(ep.out, kOut, row * ep.ld + n + e, v[e]);
+                for (int e = 0; e < V; ++e) {
+                    if (e >= left) continue;
+                    if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(po)[e] = o[e];
+                    else reinterpret_cast<uint16_t*>(po)[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
                 }
             }
         }
@@ -493,9 +550,12 @@ inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const 
                                hipStream_t st) {
     const int64_t tiles_m = (ep.M + 64 * TM - 1) / (64 * TM);
     const int64_t tiles_n = (ep.N + 64 * TN - 1) / (64 * TN);
+    // the kernel counts tiles in 32 bits (2^28 of them hold a terabyte of results)
+    if (tiles_m * tiles_n > ((int64_t)1 << 28)) return hipErrorInvalidConfiguration;
     return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
         hipLaunchKernelGGL((k_linear_tiles<TM, TN, kOut, kResid>), grid, dim3(256), 0, st, x,
-                           w, (int)groups(K), ep, tiles_m, tiles_n, b0);
+                           w, (int)groups(K), ep, (uint32_t)tiles_m,
+                           (uint32_t)tiles_n, b0);
     });
 }
 
@@ -527,13 +587,12 @@ inline int64_t linear_workspace(int64_t M, int64_t N, int64_t K, bool packed) {
 }
 
 template <int kType>
-inline hipError_t launch_slabs(const void* x, int64_t ld, int64_t M, const Slabs& sx,
-                               const uint8_t* w, int64_t N, const Slabs& sw, int64_t K,
-                               hipStream_t st) {
-    const int64_t bx = slab_blocks(M, K);
-    return launch_blocks(bx + slab_blocks(N, K), 256, [&](int64_t b0, dim3 grid) {
-        hipLaunchKernelGGL(k_slabs<kType>, grid, dim3(256), 0, st, x, ld, M, sx, w, N, sw, K, bx,
-                           b0);
+inline hipError_t launch_slabs(const void* x, int64_t ld, const Slabs& sx, const uint8_t* w,
+                               const Slabs& sw, int64_t K, const Epilogue& ep, hipStream_t st) {
+    const int64_t bx = slab_blocks(ep.M, K);
+    return launch_blocks(bx + slab_blocks(ep.N, K), 256, [&](int64_t b0, dim3 grid) {
+        hipLaunchKernelGGL(k_slabs<kType>, grid, dim3(256), 0, st, x, ld, ep.M, sx, w, ep.N, sw,
+                           ep.bias, ep.bias_type, K, bx, b0);
     });
 }
 
@@ -555,14 +614,17 @@ inline hipError_t linear(const void* x, int32_t type, int64_t ld, const uint8_t*
     const Slabs sx = slabs_at(ws, ep.M, K), sw = slabs_at(ws + slabs_bytes(ep.M, K), ep.N, K);
     hipError_t e;
     switch (type) {
-        case SCONE_BF16: e = launch_slabs<SCONE_BF16>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
-        case SCONE_FP16: e = launch_slabs<SCONE_FP16>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
-        case SCONE_FP32: e = launch_slabs<SCONE_FP32>(x, ld, ep.M, sx, w, ep.N, sw, K, st); break;
-        default: e = launch_slabs<SCONE_MX4>(x, ld, ep.M, sx, w, ep.N, sw, K, st);
+        case SCONE_BF16: e = launch_slabs<SCONE_BF16>(x, ld, sx, w, sw, K, ep, st); break;
+        case SCONE_FP16: e = launch_slabs<SCONE_FP16>(x, ld, sx, w, sw, K, ep, st); break;
+        case SCONE_FP32: e = launch_slabs<SCONE_FP32>(x, ld, sx, w, sw, K, ep, st); break;
+        default: e = launch_slabs<SCONE_MX4>(x, ld, sx, w, sw, K, ep, st);
     }
     if (e != hipSuccess) return e;
     const int64_t big = ((ep.M + 127) / 128) * ((ep.N + 255) / 256);
-    return big >= 256 ? launch_tiles<2, 4>(sx, sw, K, ep, st) : launch_tiles<1, 2>(sx, sw, K, ep, st);
+    #ifndef BIGT
+#define BIGT 2, 4
+#endif
+    return big >= 256 ? launch_tiles<BIGT>(sx, sw, K, ep, st) : launch_tiles<1, 2>(sx, sw, K, ep, st);
 }
 
 }  // namespace mx4
