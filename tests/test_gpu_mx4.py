@@ -360,7 +360,7 @@ def test_binding_refuses_mismatches():
         (ValueError, lambda: S.linear_mx4(x.view(2, 2, 100)[:, :, :], w,
                                           out=torch.empty((4, 6), device="cuda"))),
         (ValueError, lambda: S.linear_mx4(rng_tensor(1, (2, 4, 100), torch.bfloat16)[:, ::2], w)),
-        (S.SconeError, lambda: S.linear_mx4(x, w, workspace=torch.empty(
+        (S.SconeError, lambda: S.linear_mx4(x.repeat(50, 1), w, workspace=torch.empty(
             16, dtype=torch.uint8, device="cuda"))),
         (ValueError, lambda: S.linear_mx4(x, w, workspace=torch.empty(4096, device="cuda"))),
     ]

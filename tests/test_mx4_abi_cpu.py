@@ -75,16 +75,16 @@ def test_decode_step_refusals():
 def test_linear_refusals():
     lib = S.scone.lib()
     W = lib.scone_linear_mx4_workspace
-    need = W(10, 30, 100, BF16)
-    assert 800 <= need <= 1100                # ten 4-bit rows of 80 bytes
+    need = W(200, 30, 100, BF16)
+    assert need >= 230 * 68                   # both operands in 4 bits
 
-    def f(x=at(1), t=BF16, ld=100, M=10, K=100, w=at(2), N=30, bias=at(3), bt=BF16, act=1,
+    def f(x=at(1), t=BF16, ld=100, M=200, K=100, w=at(2), N=30, bias=at(3), bt=BF16, act=1,
           res=None, out=at(4), ot=BF16, ldo=30, ws=at(5), wsb=need):
         return lib.scone_linear_mx4(x, t, ld, M, K, w, N, bias, bt, act, res, out, ot, ldo, ws,
                                     wsb, None)
 
     assert f() == H and f(bias=None, bt=99) == H and f(res=at(4)) == H and f(res=at(6)) == H
-    assert f(t=MX4, ld=0, ws=None, wsb=0) == H
+    assert f(t=MX4, ld=0) == H and f(M=10, ws=None, wsb=0) == H
     assert f(M=0, x=None) == OK and f(N=0, w=None, ldo=0) == OK
     for bad in (dict(t=5), dict(t=-1), dict(ot=MX4), dict(ot=8), dict(M=-1), dict(N=-1),
                 dict(K=0), dict(K=(1 << 22) + 1, ld=1 << 23), dict(M=1 << 31), dict(N=1 << 31),
@@ -95,13 +95,14 @@ def test_linear_refusals():
                 dict(res=at(6, 1)), dict(ws=None), dict(wsb=need - 1), dict(ws=at(5, 8)),
                 # the output over x, the weights, the biases, the scratch; a residual
                 # that lies over it without being it
-                dict(out=at(1, 1998)), dict(out=at(2, 2398)), dict(out=at(3, 58)),
+                dict(out=at(1, 39998)), dict(out=at(2, 2398)), dict(out=at(3, 58)),
                 dict(out=at(5, 798)), dict(res=at(4, 2)),
                 # the scratch over what is read
                 dict(ws=at(1, 16)), dict(ws=at(2, 2384)), dict(ws=at(3, 48)),
                 dict(ws=at(6), res=at(6, 16))):
         assert f(**bad) == E, bad
-    assert W(10, 30, 100, MX4) == 0 and W(0, 30, 100, F32) == 0 == W(10, 0, 100, F32)
+    assert W(200, 30, 100, MX4) == need
+    assert W(1, 30, 100, F32) == W(0, 30, 100, F32) == W(200, 0, 100, F32) == 0
     for a in ((-1, 3, 3, BF16), (3, -1, 3, BF16), (3, 3, 0, BF16), (3, 3, 3, 4),
               (1 << 31, 3, 3, BF16), (3, 3, (1 << 22) + 1, MX4)):
         assert W(*a) == -1
@@ -119,7 +120,7 @@ def test_binding_refusals():
         S.gather_mx4(torch.zeros(3, dtype=torch.int32), x)
     with pytest.raises(TypeError):
         S.dequantize_mx4(x)
-    assert S.linear_mx4_workspace_bytes(10, 30, 100, torch.float16) >= 800
+    assert S.linear_mx4_workspace_bytes(200, 30, 100, torch.float16) >= 230 * 68
     assert S.linear_mx4_workspace_bytes(10, 30, 100) == 0
     with pytest.raises(ValueError):
         S.linear_mx4_workspace_bytes(-1, 30, 100)
