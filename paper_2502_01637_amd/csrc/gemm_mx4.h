@@ -108,45 +108,48 @@ __device__ __forceinline__ float gelu_for(float x) {
 }
 
 // Few rows of x: the weights are read once, from memory straight into the lanes, and
-// bound the time.  A workgroup of kFewWaves wavefronts takes 16 rows of w, which the
-// wavefronts split by pairs of groups (128 bytes of a row); each quantises its groups of
-// x itself, a block of 32 elements a lane, so that there is one launch and no scratch,
-// and the sums of the wavefronts are joined in LDS in their order.
-constexpr int kFewWaves = 8;
+// bound the time.  A workgroup of kFewWaves wavefronts takes 16 rows of w; a round is
+// kFewWaves groups, one a wavefront, whose weights are on their way kFewAhead rounds
+// ahead.  The workgroup quantises x itself, a chunk of rounds at a time into LDS, so that
+// there is one launch and no scratch.  The sums of the wavefronts are joined in LDS in
+// their order.
+//
+// In LDS a row's four 16-byte blocks of a group lie at slot block ^ s with s = -(row / 4)
+// mod 4: the 16 lanes of a read that are served at once (k_linear_tiles) are then four
+// rows at one block and the other twelve at the same or the next, each in its own banks.
+constexpr int kFewWaves = 8, kFewAhead = 4;
 
-// The lane's block of row m of x: 16 bytes of codes and the scale byte.
+// Rounds in LDS at once for MT * 16 rows: 34 KiB, four workgroups a compute unit.
+constexpr int few_rounds(int mt) { return 4 / mt; }
+
+// Codes and scale byte of a block of 32, elements e on of the K that begin at x[row].
 template <int kType>
-__device__ __forceinline__ void few_x(const void* __restrict__ x, int64_t ld, int64_t m, int64_t K,
-                                      int g, int rb, int k, int q, u32x4& codes, uint32_t& s) {
-    if constexpr (kType == SCONE_MX4) {
-        const uint8_t* row = static_cast<const uint8_t*>(x) + m * rb;
-        codes = *reinterpret_cast<const u32x4*>(row + k * 64 + q * 16);
-        s = row[64 * (int64_t)g + k * 4 + q];
+__device__ __forceinline__ u32x4 quantize32(const void* __restrict__ x, int64_t row, int64_t e,
+                                            int64_t K, uint32_t& s) {
+    typedef Elem<kType> E;
+    const typename E::type* p = static_cast<const typename E::type*>(x) + row;
+    typename E::vec v[4];
+    if (e + 32 <= K) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = load8<kType>(p + e + i * 8, 8);
     } else {
-        typedef Elem<kType> E;
-        const int64_t e = (int64_t)k * 128 + q * 32;
-        const typename E::type* p = static_cast<const typename E::type*>(x) + m * ld;
-        typename E::vec v[4];
-        uint32_t top = 0;
-        if (e + 32 <= K) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = load8<kType>(p + e + i * 8, 8);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t left = K - e - i * 8;
-                v[i] = load8<kType>(p + (left > 0 ? e + i * 8 : 0), left);
-            }
-        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t t = E::top(v[i]);
-            top = top > t ? top : t;
+            const int64_t left = K - e - i * 8;
+            v[i] = load8<kType>(p + (left > 0 ? e + i * 8 : 0), left);
         }
-        s = scale_byte(E::field(top));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) codes[i] = s == 255 ? 0u : E::quantize(v[i], scale_of(s));
     }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t t = E::top(v[i]);
+        top = top > t ? top : t;
+    }
+    s = scale_byte(E::field(top));
+    u32x4 codes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) codes[i] = s == 255 ? 0u : E::quantize(v[i], scale_of(s));
+    return codes;
 }
 
 template <int kType, int MT>
@@ -155,63 +158,98 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __res
                                                                const uint8_t* __restrict__ w,
                                                                int64_t K, Epilogue ep,
                                                                int64_t block0) {
-    __shared__ f32x4 part[kFewWaves][MT][16][4];  // [m][four n]
+    constexpr int kRows = 16 * MT, kRounds = few_rounds(MT), kChunk = kRounds * kFewWaves;
+    constexpr bool kQuantize = kType != SCONE_MX4;
+    // x's codes [group of the chunk][row][64] and scale words behind them; then the sums
+    // [wavefront][row][16 n]
+    constexpr int kCodes = kQuantize ? kChunk * kRows * 64 : 0;
+    constexpr int kLds = kQuantize ? kCodes + kChunk * kRows * 4 : 0;
+    constexpr int kSums = kFewWaves * kRows * 64;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[kLds > kSums ? kLds : kSums];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t n0 = block_index(block0) * 16;
     const int fr = lane & 15, q = lane >> 4;
     const int g = (int)groups(K), rb = (int)row_bytes(K);
     // Rows past the end read the last row and are not stored.
-    const uint8_t* pw = w + (n0 + fr < ep.N ? n0 + fr : ep.N - 1) * rb;
-    int64_t m[MT];
+    const uint8_t* const pw = w + (n0 + fr < ep.N ? n0 + fr : ep.N - 1) * rb;
+    const uint8_t* px[MT];
+    if constexpr (!kQuantize)
 #pragma unroll
-    for (int i = 0; i < MT; ++i) m[i] = i * 16 + fr < ep.M ? i * 16 + fr : ep.M - 1;
-    f32x4 acc[MT] = {};
-    u32x4 a[2][2];  // [this pair or the next][group]
-    uint32_t sa[2][2];
-    auto load = [&](int k, u32x4 (&v)[2], uint32_t (&s)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int at = k + u < g ? k + u : g - 1;  // a last odd group twice, once unused
-            v[u] = *reinterpret_cast<const u32x4*>(pw + at * 64 + q * 16);
-            s[u] = pw[64 * (int64_t)g + at * 4 + q];
-        }
+        for (int i = 0; i < MT; ++i)
+            px[i] = static_cast<const uint8_t*>(x) +
+                    (i * 16 + fr < ep.M ? i * 16 + fr : ep.M - 1) * rb;
+    u32x4 a[kFewAhead];
+    uint32_t sa[kFewAhead];
+    auto load = [&](int round, u32x4& v, uint32_t& s) {
+        const int k = round * kFewWaves + wave;
+        if (k >= g) return;
+        v = *reinterpret_cast<const u32x4*>(pw + k * 64 + q * 16);
+        s = pw[64 * (int64_t)g + k * 4 + q];
     };
-    auto step = [&](int k, const u32x4 (&v)[2], const uint32_t (&s)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (k + u >= g) break;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                u32x4 b;
-                uint32_t sb;
-                few_x<kType>(x, ld, m[i], K, g, rb, k + u, q, b, sb);
-                acc[i] = mfma_mx4(v[u], b, acc[i], s[u], sb);
+    // Rows of x beyond M stay as they are in LDS: they reach only rows that are not stored.
+    auto fill = [&](int k0) {
+        if constexpr (kQuantize) {
+            const int n = (g - k0 < kChunk ? g - k0 : kChunk) * 4;  // blocks of a row
+            for (int u = threadIdx.x; u < (int)ep.M * n; u += 64 * kFewWaves) {
+                const int r = u / n, c = u - r * n, k = c >> 2;
+                uint32_t s;
+                const u32x4 codes = quantize32<kType>(x, r * ld, (int64_t)(k0 * 4 + c) * 32, K, s);
+                const int slot = (c & 3) ^ (-(r >> 2) & 3);
+                *reinterpret_cast<u32x4*>(smem + (k * kRows + r) * 64 + slot * 16) = codes;
+                smem[kCodes + (k * kRows + r) * 4 + (c & 3)] = (uint8_t)s;
             }
         }
     };
-    constexpr int kStep = kFewWaves * 2;
-    int k = wave * 2;
-    if (k < g) load(k, a[0], sa[0]);
-    while (k < g) {  // the next pair's weights are on their way
-        if (k + kStep < g) load(k + kStep, a[1], sa[1]);
-        step(k, a[0], sa[0]);
-        k += kStep;
-        if (k >= g) break;
-        if (k + kStep < g) load(k + kStep, a[0], sa[0]);
-        step(k, a[1], sa[1]);
-        k += kStep;
+    f32x4 acc[MT] = {};
+    auto step = [&](int round, const u32x4& v, uint32_t s) {
+        const int k = round * kFewWaves + wave;
+        if (k >= g) return;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            u32x4 b;
+            uint32_t sb;
+            if constexpr (kQuantize) {
+                const int at = k % kChunk * kRows + i * 16 + fr;
+                b = *reinterpret_cast<const u32x4*>(smem + at * 64 +
+                                                    ((q ^ (-(fr >> 2) & 3)) * 16));
+                sb = *reinterpret_cast<const uint32_t*>(smem + kCodes + at * 4) >> (8 * q);
+            } else {
+                b = *reinterpret_cast<const u32x4*>(px[i] + k * 64 + q * 16);
+                sb = px[i][64 * (int64_t)g + k * 4 + q];
+            }
+            acc[i] = mfma_mx4(v, b, acc[i], s, sb);
+        }
+    };
+    const int rounds = (g + kFewWaves - 1) / kFewWaves;
+#pragma unroll
+    for (int j = 0; j < kFewAhead; ++j) load(j, a[j], sa[j]);
+    for (int r0 = 0; r0 < rounds; r0 += kFewAhead) {
+#pragma unroll
+        for (int j = 0; j < kFewAhead; ++j) {
+            const int r = r0 + j;
+            if (r >= rounds) break;
+            if (kQuantize && r % kRounds == 0) {
+                if (r > 0) __syncthreads();
+                fill(r * kFewWaves);
+                __syncthreads();
+            }
+            step(r, a[j], sa[j]);
+            load(r + kFewAhead, a[j], sa[j]);
+        }
     }
     // acc[i][r] is out[i * 16 + lane % 16, n0 + 4 (lane / 16) + r].
-#pragma unroll
-    for (int i = 0; i < MT; ++i) part[wave][i][fr][q] = acc[i];
     __syncthreads();
-    const float* sums = reinterpret_cast<const float*>(part);
-    for (int t = threadIdx.x; t < MT * 256; t += 64 * kFewWaves) {
+    float* const sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+        *reinterpret_cast<f32x4*>(sums + ((wave * kRows + i * 16 + fr) * 16 + q * 4)) = acc[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < kRows * 16; t += 64 * kFewWaves) {
         const int64_t row = t >> 4, n = n0 + (t & 15);
         if (row >= ep.M || n >= ep.N) continue;
         float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < kFewWaves; ++j) v += sums[j * MT * 256 + t];
+        for (int j = 0; j < kFewWaves; ++j) v += sums[j * kRows * 16 + t];
         if (ep.bias) v += load_elem(ep.bias, ep.bias_type, n);
         if (ep.gelu) v = ep.out_type == SCONE_FP32 ? gemm::gelu_erf(v) : gelu_16(v);
         if (ep.residual) v += load_elem(ep.residual, ep.out_type, row * ep.ld + n);
