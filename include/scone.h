@@ -26,7 +26,7 @@
  *  - No call allocates device memory except scone_build_fgram_table,
  *    scone_host_alloc and the synchronous offline calls
  *    scone_discover_fgrams (when given no workspace) and
- *    scone_fgram_model_forward.  The device error word is a variable of the
+ *    scone_fgram_model_forward (and its _mx4, when given no workspace).  The device error word is a variable of the
  *    library's own code object (one per GPU), not an allocation.
  *  - All buffers are owned by the caller except the table handle, which the
  *    library owns until scone_table_destroy.
@@ -584,6 +584,34 @@ int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t* lengths,
  * the call rejects. */
 int64_t scone_fgram_model_workspace(int64_t n, int32_t max_len, int32_t d, int32_t n_heads,
                                     int32_t d_ff);
+
+/*
+ * The precompute of F with the model's linear maps in 4 bits (scone_quantize_mx4 has
+ * the format): the weights of every w_qkv, w_o, w_fc1 and w_fc2 are 4-bit rows, and the
+ * bf16 inputs of those four products are rounded to 4-bit rows too (scone_linear_mx4).
+ * Everything else is as in scone_fgram_model_forward_in.
+ *
+ *  params    as there; its linear weights are not read.
+ *  weights   scone_fgram_model_mx4_bytes bytes, 16-byte aligned: per layer the 4-bit
+ *            rows of w_qkv [3d], w_o [d], w_fc1 [d_ff] and w_fc2 [d], one after another,
+ *            as scone_fgram_model_quantize writes them from params.  Sharing memory with
+ *            rows or the workspace gives SCONE_EINVAL.
+ *  workspace at least scone_fgram_model_workspace_mx4 bytes, or NULL.
+ *
+ * scone_fgram_model_quantize is asynchronous on `stream`; weights may not share memory
+ * with params (SCONE_EINVAL).  The two sizes are -1 for arguments that the calls reject.
+ */
+int scone_fgram_model_forward_mx4(const int32_t* fgrams, const int32_t* lengths,
+                                  const int32_t* row_ids, int64_t n, int32_t max_len,
+                                  const void* tok_rows, int64_t vocab, const void* params,
+                                  const void* weights, int32_t d, int32_t n_heads, int32_t d_ff,
+                                  int32_t n_layers, void* rows, int64_t n_rows, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+int scone_fgram_model_quantize(const void* params, int32_t d, int32_t n_heads, int32_t d_ff,
+                               int32_t n_layers, int32_t max_len, void* weights, void* stream);
+int64_t scone_fgram_model_mx4_bytes(int32_t d, int32_t n_heads, int32_t d_ff, int32_t n_layers);
+int64_t scone_fgram_model_workspace_mx4(int64_t n, int32_t max_len, int32_t d, int32_t n_heads,
+                                        int32_t d_ff);
 
 /*
  * Packing of scone_fgram_model_forward's parameters: offsets[k] (elements)

@@ -52,6 +52,17 @@ def values(rows: np.ndarray, cols: int) -> np.ndarray:
     return (v * np.repeat(scale, 32, axis=1))[:, :cols]
 
 
+def rounded(x: np.ndarray) -> np.ndarray:
+    """values(quantize(x)) for finite x [..., cols], cols a multiple of 32, at once."""
+    v = np.asarray(x, np.float64).reshape(-1, 32)
+    _, e = np.frexp(np.abs(v).max(axis=1, keepdims=True))       # top in [2^(e-1), 2^e)
+    scale = np.exp2(np.maximum(e - 3.0, -127.0))
+    a = np.abs(v) / scale
+    # the grid's steps: 1/2 below 2, 1 below 4, then 2; rint takes ties to even
+    step = np.where(a < 2, 0.5, np.where(a < 4, 1.0, 2.0))
+    return np.copysign(np.minimum(np.rint(a / step) * step, 6.0) * scale, v).reshape(np.shape(x))
+
+
 def linear(x: np.ndarray, w: np.ndarray, bias=None, gelu=False, residual=None):
     """act(x w^T + bias) + residual, and sum |x| |w| (what sums round relative to)."""
     y = x @ w.T
@@ -65,3 +76,31 @@ def linear(x: np.ndarray, w: np.ndarray, bias=None, gelu=False, residual=None):
     if residual is not None:
         y = y + residual
     return y, size
+
+
+def fgram_forward(fgrams, lengths, tok_emb, params, n_layers, n_heads):
+    """F's rows by a model whose linear weights and their inputs are held in 4 bits, the
+    inputs rounded to bf16 before (and q, k, v); 64 bits in between.  The model is that
+    of oracle/fgram_model.py."""
+    from . import fgram_model as m
+    d = tok_emb.shape[1]
+    W = {k: rounded(v) for k, v in params.items() if k.split(".")[-1].startswith("w_")}
+    out = np.zeros((len(lengths), d))
+    for n in np.unique(lengths):
+        sel = np.flatnonzero(lengths == n)
+        G = len(sel)
+        h = tok_emb[np.asarray(fgrams)[sel, :n]] + params["pos"][:n]
+        for l in range(n_layers):
+            p = {k.split(".")[1]: v for k, v in params.items() if k.startswith(f"l{l}.")}
+            w = {k.split(".")[1]: v for k, v in W.items() if k.startswith(f"l{l}.")}
+            a = m.round_bf16(m.layer_norm(h, p["ln1_g"], p["ln1_b"]))
+            qkv = m.round_bf16(rounded(a) @ w["w_qkv"].T + p["b_qkv"])
+            q, k, v = (qkv[..., i * d:(i + 1) * d].reshape(G, n, n_heads, d // n_heads)
+                       .transpose(0, 2, 1, 3) for i in range(3))
+            o = m.causal_attention(q, k, v).transpose(0, 2, 1, 3).reshape(G, n, d)
+            h = h + rounded(m.round_bf16(o)) @ w["w_o"].T + p["b_o"]
+            a = m.round_bf16(m.layer_norm(h, p["ln2_g"], p["ln2_b"]))
+            f = m.round_bf16(m.gelu(rounded(a) @ w["w_fc1"].T + p["b_fc1"]))
+            h = h + rounded(f) @ w["w_fc2"].T + p["b_fc2"]
+        out[sel] = m.layer_norm(h[:, n - 1], params["lnf_g"], params["lnf_b"])
+    return out

@@ -38,6 +38,7 @@
 
 #include <algorithm>
 #include <new>
+#include <utility>
 #include <vector>
 
 namespace scone {
@@ -312,6 +313,8 @@ struct Weights {
     struct Layer {
         const uint16_t *ln1_g, *ln1_b, *w_qkv, *b_qkv, *w_o, *b_o, *ln2_g, *ln2_b, *w_fc1,
             *b_fc1, *w_fc2, *b_fc2;
+        // the four linear maps' weights as 4-bit rows, or null
+        const uint8_t *q_qkv = nullptr, *q_o = nullptr, *q_fc1 = nullptr, *q_fc2 = nullptr;
     };
     std::vector<Layer> layers;
     const uint16_t *lnf_g, *lnf_b;
@@ -340,13 +343,40 @@ Weights bind_weights(const uint16_t* blob, int64_t d, int64_t d_ff, int n_layers
     return w;
 }
 
+// Bytes of a layer's 4-bit weights: qkv, o, fc1, fc2, each row by row.
+int64_t mx4_layer_bytes(int64_t d, int64_t d_ff) {
+    return (4 * d + d_ff) * mx4::row_bytes(d) + d * mx4::row_bytes(d_ff);
+}
+
+void bind_mx4(Weights& w, const uint8_t* blob, int64_t d, int64_t d_ff) {
+    for (Weights::Layer& L : w.layers) {
+        L.q_qkv = blob;
+        L.q_o = L.q_qkv + 3 * d * mx4::row_bytes(d);
+        L.q_fc1 = L.q_o + d * mx4::row_bytes(d);
+        L.q_fc2 = L.q_fc1 + d_ff * mx4::row_bytes(d);
+        blob += mx4_layer_bytes(d, d_ff);
+    }
+}
+
 // ------------------------------------------------------------------ driver --
 
 struct Buffers {
     Node* nodes;
     float* h;
     uint16_t *a, *qkv, *f;
+    uint8_t* mx4;  // the 4-bit products' scratch
 };
+
+// out = epilogue(x W^T + b), W in bf16 or, where the model has them, in 4 bits (then x is
+// rounded to 4 bits too).  kResid adds to out (fp32), the others write bf16.
+template <gemm::Epilogue EPI>
+hipError_t product(const uint16_t* x, const uint16_t* w, const uint8_t* q, const uint16_t* b,
+                   void* out, int M, int N, int K, const Buffers& B, hipStream_t st) {
+    if (!q) return gemm::launch<EPI>(x, w, b, out, N, M, N, K, st);
+    const mx4::Epilogue ep{b, EPI == gemm::kResid ? out : nullptr, out, N, M, N, SCONE_BF16,
+                           EPI == gemm::kResid ? SCONE_FP32 : SCONE_BF16, EPI == gemm::kGelu};
+    return mx4::linear(x, SCONE_BF16, K, q, K, ep, B.mx4, st);
+}
 
 // One chunk whose nodes are in B.nodes; `order` holds its f-grams.
 template <int R>
@@ -371,7 +401,7 @@ hipError_t run_chunk(const Weights& w, const int32_t* order, const Chunk& c,
         if (l > 0)
             hipLaunchKernelGGL(k_ln<R>, dim3(g_rows), dim3(kThreads), 0, st, B.h, M, L.ln1_g,
                                L.ln1_b, B.a);
-        e = gemm::launch<gemm::kBias>(B.a, L.w_qkv, L.b_qkv, B.qkv, 3 * d, (int)M, 3 * d, d, st);
+        e = product<gemm::kBias>(B.a, L.w_qkv, L.q_qkv, L.b_qkv, B.qkv, (int)M, 3 * d, d, B, st);
         if (e != hipSuccess) break;
         // Only the f-grams' last tokens reach F, so from the last layer's
         // attention on, the first n_f rows are all that is computed.
@@ -380,13 +410,13 @@ hipError_t run_chunk(const Weights& w, const int32_t* order, const Chunk& c,
         // attention output overwrites a (its input to the qkv product is consumed)
         e = attention(B.qkv, B.a, Mr, d, dh, scale, B.nodes, st);
         if (e != hipSuccess) break;
-        e = gemm::launch<gemm::kResid>(B.a, L.w_o, L.b_o, B.h, d, (int)Mr, d, d, st);
+        e = product<gemm::kResid>(B.a, L.w_o, L.q_o, L.b_o, B.h, (int)Mr, d, d, B, st);
         if (e != hipSuccess) break;
         hipLaunchKernelGGL(k_ln<R>, dim3(g_r), dim3(kThreads), 0, st, B.h, Mr, L.ln2_g, L.ln2_b,
                            B.a);
-        e = gemm::launch<gemm::kGelu>(B.a, L.w_fc1, L.b_fc1, B.f, d_ff, (int)Mr, d_ff, d, st);
+        e = product<gemm::kGelu>(B.a, L.w_fc1, L.q_fc1, L.b_fc1, B.f, (int)Mr, d_ff, d, B, st);
         if (e != hipSuccess) break;
-        e = gemm::launch<gemm::kResid>(B.f, L.w_fc2, L.b_fc2, B.h, d, (int)Mr, d, d_ff, st);
+        e = product<gemm::kResid>(B.f, L.w_fc2, L.q_fc2, L.b_fc2, B.h, (int)Mr, d, d_ff, B, st);
     }
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_final<R>, dim3(g_f), dim3(kThreads), 0, st, B.h, order, n_f, row_ids,
@@ -398,10 +428,10 @@ hipError_t run_chunk(const Weights& w, const int32_t* order, const Chunk& c,
 // activations of one chunk.
 struct ModelLayout {
     tree::Layout tree;
-    size_t h, a, qkv, f, total;
+    size_t h, a, qkv, f, mx4, total;
 };
 
-ModelLayout model_layout(int64_t n, int max_len, int64_t d, int64_t d_ff) {
+ModelLayout model_layout(int64_t n, int max_len, int64_t d, int64_t d_ff, bool mx4) {
     ModelLayout l{};
     l.tree = tree::layout(n, max_len);
     size_t off = l.tree.total;
@@ -417,6 +447,13 @@ ModelLayout model_layout(int64_t n, int max_len, int64_t d, int64_t d_ff) {
     l.a = take((size_t)(padded * d) * 2);
     l.qkv = take((size_t)(rows * 3 * d) * 2);
     l.f = take((size_t)(padded * d_ff) * 2);
+    if (mx4) {  // the largest of the four products' scratch, for any number of rows up to these
+        int64_t most = 0;
+        for (const auto& nk : {std::pair<int64_t, int64_t>{3 * d, d}, {d, d}, {d_ff, d}, {d, d_ff}})
+            most = std::max(most, mx4::slabs_bytes(rows, nk.second) +
+                                      mx4::slabs_bytes(nk.first, nk.second));
+        l.mx4 = take((size_t)most);
+    }
     l.total = off;
     return l;
 }
@@ -462,7 +499,21 @@ extern "C" int64_t scone_fgram_model_workspace(int64_t n, int32_t max_len, int32
                                                int32_t n_heads, int32_t d_ff) {
     using namespace scone;
     if (!dims_ok(d, n_heads, d_ff, 0, max_len) || n < 0 || n > 0x7fffffffLL) return -1;
-    return (int64_t)model_layout(n, max_len, d, d_ff).total;
+    return (int64_t)model_layout(n, max_len, d, d_ff, false).total;
+}
+
+extern "C" int64_t scone_fgram_model_workspace_mx4(int64_t n, int32_t max_len, int32_t d,
+                                                   int32_t n_heads, int32_t d_ff) {
+    using namespace scone;
+    if (!dims_ok(d, n_heads, d_ff, 0, max_len) || n < 0 || n > 0x7fffffffLL) return -1;
+    return (int64_t)model_layout(n, max_len, d, d_ff, true).total;
+}
+
+extern "C" int64_t scone_fgram_model_mx4_bytes(int32_t d, int32_t n_heads, int32_t d_ff,
+                                               int32_t n_layers) {
+    using namespace scone;
+    if (!dims_ok(d, n_heads, d_ff, n_layers, 2)) return -1;
+    return n_layers * mx4_layer_bytes(d, d_ff);
 }
 
 namespace scone {
@@ -471,24 +522,26 @@ namespace {
 // Everything after the argument checks, in a workspace of model_layout's size.
 int run_model(const int32_t* fgrams, const int32_t* lengths, const int32_t* row_ids, int64_t n,
               int32_t max_len, const uint16_t* tok_rows, int64_t vocab, const uint16_t* params,
-              int32_t d, int32_t n_heads, int32_t d_ff, int32_t n_layers, uint16_t* rows,
-              int64_t n_rows, uint8_t* ws, hipStream_t st) {
+              const uint8_t* weights, int32_t d, int32_t n_heads, int32_t d_ff, int32_t n_layers,
+              uint16_t* rows, int64_t n_rows, uint8_t* ws, hipStream_t st) {
     const ChunkFn fn = chunk_fn(d);
     if (!fn) return SCONE_EINVAL;
-    const ModelLayout lay = model_layout(n, max_len, d, d_ff);
+    const ModelLayout lay = model_layout(n, max_len, d, d_ff, weights != nullptr);
     const tree::Builder tb{fgrams, lengths, n, max_len, vocab, ws, lay.tree, n_layers == 0, st};
     std::vector<Chunk> chunks;
     unsigned bits = 0;
     const int rc = tb.build(chunks, bits);
     if (rc != SCONE_OK) return rc;
     if (bits & err_bit(SCONE_ELEN)) return SCONE_ELEN;
-    const Weights w = bind_weights(params, d, d_ff, n_layers, max_len);
+    Weights w = bind_weights(params, d, d_ff, n_layers, max_len);
+    if (weights) bind_mx4(w, weights, d, d_ff);
     Buffers B;
     B.nodes = tb.nodes();
     B.h = reinterpret_cast<float*>(ws + lay.h);
     B.a = reinterpret_cast<uint16_t*>(ws + lay.a);
     B.qkv = reinterpret_cast<uint16_t*>(ws + lay.qkv);
     B.f = reinterpret_cast<uint16_t*>(ws + lay.f);
+    B.mx4 = weights ? ws + lay.mx4 : nullptr;
     for (const Chunk& c : chunks) {
         if (tb.fill_nodes(c) != hipSuccess ||
             fn(w, tb.order() + c.first, c, tok_rows, d_ff, n_heads, row_ids, rows, n_rows, B,
@@ -506,19 +559,20 @@ int run_model(const int32_t* fgrams, const int32_t* lengths, const int32_t* row_
 }  // namespace
 }  // namespace scone
 
-extern "C" int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t* lengths,
-                                            const int32_t* row_ids, int64_t n, int32_t max_len,
-                                            const void* tok_rows, int64_t vocab,
-                                            const void* params, int32_t d, int32_t n_heads,
-                                            int32_t d_ff, int32_t n_layers, void* rows,
-                                            int64_t n_rows, void* workspace,
-                                            int64_t workspace_bytes, void* stream) {
-    using namespace scone;
+namespace scone {
+namespace {
+
+// The whole of scone_fgram_model_forward_in, with `weights` that of ..._mx4.
+int forward_in(const int32_t* fgrams, const int32_t* lengths, const int32_t* row_ids, int64_t n,
+               int32_t max_len, const void* tok_rows, int64_t vocab, const void* params,
+               const void* weights, int32_t d, int32_t n_heads, int32_t d_ff, int32_t n_layers,
+               void* rows, int64_t n_rows, void* workspace, int64_t workspace_bytes,
+               void* stream) {
     if (!dims_ok(d, n_heads, d_ff, n_layers, max_len)) return SCONE_EINVAL;
     if (n < 0 || vocab <= 0 || n_rows < 0 || n > 0x7fffffffLL) return SCONE_EINVAL;
     if (n == 0) return SCONE_OK;
     if (!fgrams || !lengths || !row_ids || !tok_rows || !params || !rows) return SCONE_EINVAL;
-    if (((uintptr_t)tok_rows | (uintptr_t)params | (uintptr_t)rows) % 16 != 0)
+    if (((uintptr_t)tok_rows | (uintptr_t)params | (uintptr_t)rows | (uintptr_t)weights) % 16 != 0)
         return SCONE_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     void* own = nullptr;
@@ -528,21 +582,22 @@ extern "C" int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t
         // f-grams, lengths, row ids and parameters: `rows` may share memory
         // with none of them (tok_rows may lie inside it, as documented), and
         // the workspace with nothing at all.
-        const size_t need = model_layout(n, max_len, d, d_ff).total;
+        const size_t need = model_layout(n, max_len, d, d_ff, weights != nullptr).total;
         int64_t p_elems = 0;
         for (int64_t e : param_sizes(d, d_ff, n_layers, max_len)) p_elems += align_up(e);
-        const void* buf[6] = {fgrams, lengths, row_ids, params, rows, tok_rows};
-        const int64_t len[6] = {span_bytes(n, 4 * (int64_t)max_len), span_bytes(n, 4),
+        const void* buf[7] = {fgrams, lengths, row_ids, params, weights, rows, tok_rows};
+        const int64_t len[7] = {span_bytes(n, 4 * (int64_t)max_len), span_bytes(n, 4),
                                 span_bytes(n, 4), span_bytes(p_elems, 2),
+                                n_layers * mx4_layer_bytes(d, d_ff),
                                 span_bytes(n_rows, 2 * (int64_t)d),
                                 span_bytes(vocab, 2 * (int64_t)d)};
-        for (int i = 0; i < 4; ++i)
-            if (overlaps(rows, len[4], buf[i], len[i])) return SCONE_EINVAL;
+        for (int i = 0; i < 5; ++i)
+            if (overlaps(rows, len[5], buf[i], len[i])) return SCONE_EINVAL;
         if (workspace) {
             if (workspace_bytes < 0 || (uint64_t)workspace_bytes < need ||
                 (uintptr_t)workspace % 256 != 0)
                 return SCONE_EINVAL;
-            for (int i = 0; i < 6; ++i)
+            for (int i = 0; i < 7; ++i)
                 if (overlaps(workspace, (int64_t)need, buf[i], len[i])) return SCONE_EINVAL;
         } else {
             if (hipMalloc(&own, need) != hipSuccess) {
@@ -553,7 +608,8 @@ extern "C" int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t
         }
         rc = run_model(fgrams, lengths, row_ids, n, max_len,
                        static_cast<const uint16_t*>(tok_rows), vocab,
-                       static_cast<const uint16_t*>(params), d, n_heads, d_ff, n_layers,
+                       static_cast<const uint16_t*>(params),
+                       static_cast<const uint8_t*>(weights), d, n_heads, d_ff, n_layers,
                        static_cast<uint16_t*>(rows), n_rows, static_cast<uint8_t*>(workspace),
                        st);
     } catch (const std::bad_alloc&) {
@@ -563,6 +619,68 @@ extern "C" int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t
     if (rc != SCONE_OK) (void)hipStreamSynchronize(st);
     if (own) (void)hipFree(own);
     return rc;
+}
+
+}  // namespace
+}  // namespace scone
+
+extern "C" int scone_fgram_model_forward_in(const int32_t* fgrams, const int32_t* lengths,
+                                            const int32_t* row_ids, int64_t n, int32_t max_len,
+                                            const void* tok_rows, int64_t vocab,
+                                            const void* params, int32_t d, int32_t n_heads,
+                                            int32_t d_ff, int32_t n_layers, void* rows,
+                                            int64_t n_rows, void* workspace,
+                                            int64_t workspace_bytes, void* stream) {
+    return scone::forward_in(fgrams, lengths, row_ids, n, max_len, tok_rows, vocab, params,
+                             nullptr, d, n_heads, d_ff, n_layers, rows, n_rows, workspace,
+                             workspace_bytes, stream);
+}
+
+extern "C" int scone_fgram_model_forward_mx4(const int32_t* fgrams, const int32_t* lengths,
+                                             const int32_t* row_ids, int64_t n, int32_t max_len,
+                                             const void* tok_rows, int64_t vocab,
+                                             const void* params, const void* weights, int32_t d,
+                                             int32_t n_heads, int32_t d_ff, int32_t n_layers,
+                                             void* rows, int64_t n_rows, void* workspace,
+                                             int64_t workspace_bytes, void* stream) {
+    if (!weights && n != 0) return SCONE_EINVAL;
+    return scone::forward_in(fgrams, lengths, row_ids, n, max_len, tok_rows, vocab, params,
+                             weights, d, n_heads, d_ff, n_layers, rows, n_rows, workspace,
+                             workspace_bytes, stream);
+}
+
+extern "C" int scone_fgram_model_quantize(const void* params, int32_t d, int32_t n_heads,
+                                          int32_t d_ff, int32_t n_layers, int32_t max_len,
+                                          void* weights, void* stream) {
+    using namespace scone;
+    if (!dims_ok(d, n_heads, d_ff, n_layers, max_len)) return SCONE_EINVAL;
+    if (n_layers == 0) return SCONE_OK;
+    if (!params || !weights || ((uintptr_t)params | (uintptr_t)weights) % 16 != 0)
+        return SCONE_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    try {
+        int64_t p_elems = 0;
+        for (int64_t e : param_sizes(d, d_ff, n_layers, max_len)) p_elems += align_up(e);
+        if (overlaps(weights, n_layers * mx4_layer_bytes(d, d_ff), params, 2 * p_elems))
+            return SCONE_EINVAL;
+        Weights w = bind_weights(static_cast<const uint16_t*>(params), d, d_ff, n_layers, max_len);
+        bind_mx4(w, static_cast<const uint8_t*>(weights), d, d_ff);
+        for (const Weights::Layer& L : w.layers) {
+            const struct { const uint16_t* from; const uint8_t* to; int64_t n, cols; } part[4] = {
+                {L.w_qkv, L.q_qkv, 3 * (int64_t)d, d},
+                {L.w_o, L.q_o, d, d},
+                {L.w_fc1, L.q_fc1, d_ff, d},
+                {L.w_fc2, L.q_fc2, d, d_ff}};
+            for (const auto& p : part) {
+                const hipError_t e = mx4::quantize(p.from, SCONE_BF16, p.n, p.cols, p.cols,
+                                                   const_cast<uint8_t*>(p.to), st);
+                if (e != hipSuccess) return status_of(e);
+            }
+        }
+    } catch (const std::bad_alloc&) {
+        return SCONE_ENOMEM;
+    }
+    return SCONE_OK;
 }
 
 extern "C" int scone_fgram_model_forward(const int32_t* fgrams, const int32_t* lengths,

@@ -101,6 +101,15 @@ def _declare(L):
     L.scone_linear_mx4.argtypes = [P, I32, I64, I64, I64, P, I64, P, I32, I32, P, P, I32, I64, P,
                                    I64, P]
     L.scone_linear_mx4.restype = I
+    L.scone_fgram_model_forward_mx4.argtypes = [P, P, P, I64, I32, P, I64, P, P, I32, I32, I32,
+                                                I32, P, I64, P, I64, P]
+    L.scone_fgram_model_forward_mx4.restype = I
+    L.scone_fgram_model_quantize.argtypes = [P, I32, I32, I32, I32, I32, P, P]
+    L.scone_fgram_model_quantize.restype = I
+    L.scone_fgram_model_mx4_bytes.argtypes = [I32, I32, I32, I32]
+    L.scone_fgram_model_mx4_bytes.restype = I64
+    L.scone_fgram_model_workspace_mx4.argtypes = [I64, I32, I32, I32, I32]
+    L.scone_fgram_model_workspace_mx4.restype = I64
     L.scone_linear_mx4_workspace.argtypes = [I64, I64, I64, I32]
     L.scone_linear_mx4_workspace.restype = I64
     L.scone_host_alloc.argtypes = [I64, ctypes.POINTER(P), ctypes.POINTER(P)]
@@ -410,11 +419,32 @@ class FgramModel:
         self.device = device
 
 
+class FgramModelMx4(FgramModel):
+    """An f-gram model whose linear maps have 4-bit weights (scone_fgram_model_quantize),
+    made from a FgramModel; its other parameters are shared with that model.
+    precompute_fgram_rows rounds the inputs of its products to 4 bits too.  Returns
+    when the weights are written, so that any stream may use them."""
+
+    def __init__(self, model: FgramModel, stream=None):
+        self.d, self.n_heads, self.d_ff = model.d, model.n_heads, model.d_ff
+        self.n_layers, self.max_len = model.n_layers, model.max_len
+        self.blob, self.device = model.blob, model.blob.device
+        n = lib().scone_fgram_model_mx4_bytes(self.d, self.n_heads, self.d_ff, self.n_layers)
+        self.weights = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        with _on(self.device):
+            rc = lib().scone_fgram_model_quantize(
+                self.blob.data_ptr(), self.d, self.n_heads, self.d_ff, self.n_layers,
+                self.max_len, self.weights.data_ptr(), _stream(stream))
+            _check(rc, "scone_fgram_model_quantize")
+            torch.cuda.synchronize()
+
+
 def precompute_fgram_rows(model: FgramModel, fgrams: torch.Tensor, lengths: torch.Tensor,
                           row_ids: torch.Tensor, tok_rows: torch.Tensor, rows: torch.Tensor,
                           stream=None):
     """scone_fgram_model_forward: rows[row_ids[k]] = F(f-gram k) (bf16), the
-    f-gram model's output at the last token.  tok_rows [vocab, d] bf16 is the
+    f-gram model's output at the last token (scone_fgram_model_forward_mx4 for a
+    FgramModelMx4).  tok_rows [vocab, d] bf16 is the
     token embedding layer; rows [n_rows, d] bf16 is written in place.
     Synchronous."""
     _dev_i32(fgrams, "fgrams", 2)
@@ -427,15 +457,20 @@ def precompute_fgram_rows(model: FgramModel, fgrams: torch.Tensor, lengths: torc
     n, K = fgrams.shape
     if K != model.max_len or lengths.numel() != n or row_ids.numel() != n:
         raise ValueError("fgrams must be [n, max_len] with n lengths and n row ids")
+    mx4 = isinstance(model, FgramModelMx4)
     with _on(rows.device):
-        need = lib().scone_fgram_model_workspace(n, model.max_len, model.d, model.n_heads,
-                                                 model.d_ff)
+        workspace_bytes = lib().scone_fgram_model_workspace_mx4 if mx4 else \
+            lib().scone_fgram_model_workspace
+        need = workspace_bytes(n, model.max_len, model.d, model.n_heads, model.d_ff)
         work = _scratch(need, rows.device, stream) if n > 0 and need > 0 else None
-        rc = lib().scone_fgram_model_forward_in(
-            _ptr(fgrams), _ptr(lengths), _ptr(row_ids), n, model.max_len, _ptr(tok_rows),
-            tok_rows.shape[0], model.blob.data_ptr(), model.d, model.n_heads, model.d_ff,
-            model.n_layers, _ptr(rows), rows.shape[0], _ptr(work),
-            0 if work is None else work.numel(), _stream(stream))
+        head = (_ptr(fgrams), _ptr(lengths), _ptr(row_ids), n, model.max_len, _ptr(tok_rows),
+                tok_rows.shape[0], model.blob.data_ptr())
+        tail = (model.d, model.n_heads, model.d_ff, model.n_layers, _ptr(rows), rows.shape[0],
+                _ptr(work), 0 if work is None else work.numel(), _stream(stream))
+        if mx4:
+            rc = lib().scone_fgram_model_forward_mx4(*head, model.weights.data_ptr(), *tail)
+        else:
+            rc = lib().scone_fgram_model_forward_in(*head, *tail)
     _check(rc, "scone_fgram_model_forward")
     return rows
 

@@ -126,3 +126,33 @@ def test_binding_refusals():
         S.linear_mx4_workspace_bytes(-1, 30, 100)
     with pytest.raises(TypeError):
         S.linear_mx4_workspace_bytes(1, 30, 100, torch.int32)
+
+
+def test_model_refusals():
+    L = S.scone.lib()
+    Q, F = L.scone_fgram_model_quantize, L.scone_fgram_model_forward_mx4
+    B, W = L.scone_fgram_model_mx4_bytes, L.scone_fgram_model_workspace_mx4
+    row = 16 * 17                                     # 512 elements
+    assert B(512, 8, 1024, 3) == 3 * ((4 * 512 + 1024) * row + 512 * 2 * row)
+    assert B(512, 8, 1024, 0) == 0
+    assert B(500, 8, 1024, 1) == B(512, 8, 1000, 1) == B(512, 8, 1024, -1) == -1
+    assert W(100, 3, 512, 8, 1024) > L.scone_fgram_model_workspace(100, 3, 512, 8, 1024)
+    assert W(-1, 3, 512, 8, 1024) == W(100, 9, 512, 8, 1024) == -1
+    n = B(512, 8, 1024, 2)
+    assert Q(at(1), 512, 8, 1024, 2, 3, at(2), None) == H
+    assert Q(None, 512, 8, 1024, 0, 3, None, None) == OK
+    for bad in ((None, 512, 8, 1024, 2, 3, at(2)), (at(1), 512, 8, 1024, 2, 3, None),
+                (at(1), 500, 8, 1024, 2, 3, at(2)), (at(1), 512, 8, 1024, 2, 8, at(2)),
+                (at(1, 8), 512, 8, 1024, 2, 3, at(2)), (at(1), 512, 8, 1024, 2, 3, at(2, 4)),
+                (at(1), 512, 8, 1024, 2, 3, at(1, 4096))):
+        assert Q(*bad, None) == E, bad
+
+    def f(n=5, weights=at(5), rows=at(6), ws=at(7), wsb=1 << 34, params=at(4)):
+        return F(at(1), at(2), at(3), n, 3, at(8), 100, params, weights, 512, 8, 1024, 2, rows, 90,
+                 ws, wsb, None)
+
+    assert f(n=0, weights=None) == OK
+    for bad in (dict(weights=None), dict(weights=at(5, 8)), dict(rows=at(5, n - 16)),
+                dict(ws=at(5, -256)), dict(wsb=1000), dict(ws=at(7, 16)), dict(n=-1),
+                dict(params=None)):
+        assert f(**bad) == E, bad

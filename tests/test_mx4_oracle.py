@@ -45,3 +45,11 @@ def test_edges_of_the_scale():
         assert r[0, 64] == 255 and (r[0, :16] == 0).all() and r[0, 65] == 126
         v = mx4.values(r, 42)
         assert np.isnan(v[0, :32]).all() and (v[0, 32:] == 2.0).all()
+
+
+def test_the_vectorised_rounding_is_the_packed_one():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((9, 96)) * np.exp2(rng.integers(-20, 20, (9, 1)))
+    x[3] = 0.0
+    x[4, :9] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -7.5]
+    assert np.array_equal(mx4.rounded(x), mx4.values(mx4.quantize(x), 96))
