@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import os
 import threading
@@ -132,6 +133,8 @@ def _declare(L):
 def lib():
     """The loaded library; raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -152,7 +155,10 @@ def _check(rc: int, what: str):
 # took 13.1 us, now 8.2, a 16 x 512 prefill 13.6, now 9.0.
 # (A torch built without GPU support has no such function; nothing that needs a
 # stream runs there, but the package imports.)
+# torch.cuda.current_device() looks whether the GPU is initialised first (0.26 us, the
+# query itself 0.06); where there are CUDA tensors it is.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 _HERE = contextlib.nullcontext()
 
 
@@ -688,6 +694,7 @@ def gather_split(fgram_ids: torch.Tensor, near_rows: torch.Tensor, far_rows: "Ho
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 
 
+@functools.lru_cache(maxsize=None)
 def mx4_row_bytes(cols: int) -> int:
     """Bytes of a 4-bit row of `cols` elements (scone_mx4_row_bytes)."""
     n = int(lib().scone_mx4_row_bytes(int(cols)))
@@ -701,89 +708,103 @@ class Mx4Rows:
     scales, mx4_row_bytes(cols) bytes per row (include/scone.h has the layout).
 
     ``data`` is a contiguous CUDA uint8 tensor [n_rows, mx4_row_bytes(cols)], or a
-    HostRows of such rows in pinned host memory.  The calls that move rows as bytes
-    (gather, embed, gather_split, ...) take ``data``."""
+    HostRows of such rows in pinned host memory (``device`` is then None).  The calls
+    that move rows as bytes (gather, embed, gather_split, ...) take ``data``."""
+
+    __slots__ = ("data", "cols", "row_bytes", "placement", "n_rows", "device", "ptr")
 
     def __init__(self, data, cols: int):
-        self.cols = int(cols)
-        self.row_bytes = mx4_row_bytes(self.cols)
-        placement, ptr, n_rows, row_bytes, row_shape, dtype = _rows_arg(data)
-        if dtype != torch.uint8 or row_shape != (self.row_bytes,):
-            raise ValueError(f"data must be uint8 rows of {self.row_bytes} bytes")
+        row_bytes = mx4_row_bytes(int(cols))
+        placement, ptr, n_rows, width, row_shape, dtype = _rows_arg(data)
+        if dtype != torch.uint8 or row_shape != (row_bytes,):
+            raise ValueError(f"data must be uint8 rows of {row_bytes} bytes")
         if ptr is not None and ptr % 16:
             raise ValueError("data must be 16-byte aligned")
-        self.data = data
-        self.placement, self.n_rows = placement, n_rows
+        self.data, self.cols, self.row_bytes = data, int(cols), row_bytes
+        self.placement, self.n_rows, self.ptr = placement, n_rows, ptr
+        self.device = data.device if placement == PLACE_HBM else None
 
-    @property
-    def device(self) -> Optional[torch.device]:
-        """The tensor's device; None for rows in host memory."""
-        return self.data.device if self.placement == PLACE_HBM else None
+    @classmethod
+    def empty(cls, n_rows: int, cols: int, device) -> "Mx4Rows":
+        """Room for n_rows rows on a CUDA device."""
+        return cls(torch.empty((n_rows, mx4_row_bytes(cols)), dtype=torch.uint8, device=device),
+                   cols)
 
     @property
     def nbytes(self) -> int:
         return self.n_rows * self.row_bytes
 
-    @property
-    def ptr(self) -> Optional[int]:
-        return _ptr(self.data) if self.placement == PLACE_HBM else self.data.device_ptr
 
-
-def _mx4_arg(rows, name: str, device: Optional[torch.device] = None) -> Mx4Rows:
+def _mx4_arg(rows, name: str, device: Optional[torch.device] = None):
     if not isinstance(rows, Mx4Rows):
         raise TypeError(f"{name} must be Mx4Rows")
     if device is not None and rows.device is not None and rows.device != device:
         raise ValueError(f"{name} must be on {device}")
-    return rows
 
 
 def _float_type(dtype, name: str) -> int:
-    if dtype not in _TYPES:
+    code = _TYPES.get(dtype)
+    if code is None:
         raise TypeError(f"{name} must be bfloat16, float16 or float32, got {dtype}")
-    return _TYPES[dtype]
+    return code
 
 
-def _float_matrix(x, name: str) -> int:
-    """The row stride of a CUDA float matrix whose rows are contiguous."""
+def _run(what: str, index: int, stream, call, *args):
+    """call(*args, stream) on GPU `index`; the status is checked."""
+    if index == _current_device():
+        rc = call(*args, _raw_stream(index) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, _stream(stream))
+    if rc != OK:
+        raise SconeError(rc, what)
+
+
+def _float_rows(x, name: str, dims: Optional[int] = None):
+    """(scone_type, rows, columns, row stride) of a CUDA float matrix whose rows are
+    contiguous, or of a contiguous tensor as the matrix of its last dimension."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    _float_type(x.dtype, name)
-    if x.dim() != 2:
-        raise ValueError(f"{name} must have 2 dimensions")
-    n, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    code = _float_type(x.dtype, name)
+    shape = x.shape
+    if len(shape) < 1 or (dims is not None and len(shape) != dims):
+        raise ValueError(f"{name} must have {dims or 'some'} dimensions")
+    cols = shape[-1]
+    if x.is_contiguous():
+        n = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+        return code, n, cols, max(cols, 1)
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be contiguous, or a matrix with contiguous rows")
+    ld, step = x.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    if n > 1 and x.stride(0) < cols:
+    n = shape[0]
+    if n > 1 and ld < cols:
         raise ValueError(f"{name} must have rows that do not overlap")
-    return x.stride(0) if n > 1 else max(cols, 1)
+    return code, n, cols, ld if n > 1 else max(cols, 1)
 
 
 def quantize_mx4(x: torch.Tensor, out: Optional[Mx4Rows] = None, stream=None) -> Mx4Rows:
     """scone_quantize_mx4: the rows of x [n, cols] (bfloat16, float16 or float32, any
     row stride) in 4 bits."""
-    ld = _float_matrix(x, "x")
-    n, cols = x.shape
+    code, n, cols, ld = _float_rows(x, "x", 2)
     if out is None:
-        out = Mx4Rows(torch.empty((n, mx4_row_bytes(cols)), dtype=torch.uint8, device=x.device),
-                      cols)
-    _mx4_arg(out, "out", x.device)
-    if out.placement != PLACE_HBM or out.n_rows != n or out.cols != cols:
-        raise ValueError("out must be device rows of x's shape")
-    with _on(x.device):
-        rc = lib().scone_quantize_mx4(_ptr(x), _TYPES[x.dtype], n, cols, ld, out.ptr,
-                                      _stream(stream))
-    _check(rc, "scone_quantize_mx4")
+        out = Mx4Rows.empty(n, cols, x.device)
+    else:
+        _mx4_arg(out, "out", x.device)
+        if out.placement != PLACE_HBM or out.n_rows != n or out.cols != cols:
+            raise ValueError("out must be device rows of x's shape")
+    _run("scone_quantize_mx4", x.get_device(), stream, lib().scone_quantize_mx4,
+         x.data_ptr(), code, n, cols, ld, out.ptr)
     return out
 
 
-def gather_mx4(fgram_ids: Optional[torch.Tensor], rows: Mx4Rows,
-               dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
-               stream=None) -> torch.Tensor:
+def gather_mx4(fgram_ids: torch.Tensor, rows: Mx4Rows, dtype: torch.dtype = torch.bfloat16,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """scone_gather_mx4: out[k] = the values of rows[fgram_ids[k]] in `dtype` (that of
     `out` when given)."""
     _dev_i32(fgram_ids, "fgram_ids")
-    return _gather_mx4(fgram_ids, tuple(fgram_ids.shape), fgram_ids.device, rows, dtype, out,
-                       stream)
+    return _gather_mx4(fgram_ids, fgram_ids.shape, fgram_ids.device, rows, dtype, out, stream)
 
 
 def dequantize_mx4(rows: Mx4Rows, dtype: torch.dtype = torch.bfloat16,
@@ -798,21 +819,20 @@ def dequantize_mx4(rows: Mx4Rows, dtype: torch.dtype = torch.bfloat16,
 
 def _gather_mx4(ids, shape, device, rows, dtype, out, stream):
     _mx4_arg(rows, "rows", device)
+    cols = rows.cols
     if out is None:
-        _float_type(dtype, "dtype")
-        out = torch.empty(shape + (rows.cols,), dtype=dtype, device=device)
+        code = _float_type(dtype, "dtype")
+        out = torch.empty((*shape, cols), dtype=dtype, device=device)
+        n_tok = math.prod(shape)
     else:
-        dtype = out.dtype
-        _float_type(dtype, "out")
+        code = _float_type(out.dtype, "out")
         if out.device != device:
             raise ValueError(f"out must be on {device}")
-    n_tok = math.prod(shape)
-    if not out.is_contiguous() or out.numel() != n_tok * rows.cols:
-        raise ValueError("out must be contiguous with n_tok * cols elements")
-    with _on(device):
-        rc = lib().scone_gather_mx4(_ptr(ids), n_tok, rows.ptr, rows.n_rows, rows.cols, _ptr(out),
-                                    _TYPES[dtype], rows.placement, _stream(stream))
-    _check(rc, "scone_gather_mx4")
+        n_tok = math.prod(shape)
+        if not out.is_contiguous() or out.numel() != n_tok * cols:
+            raise ValueError("out must be contiguous with n_tok * cols elements")
+    _run("scone_gather_mx4", out.get_device(), stream, lib().scone_gather_mx4, _ptr(ids), n_tok,
+         rows.ptr, rows.n_rows, cols, out.data_ptr(), code, rows.placement)
     return out
 
 
@@ -828,23 +848,21 @@ def decode_step_mx4(table: Table, ctx: torch.Tensor, ctx_len: torch.Tensor, new_
     S, cap = ctx.shape
     if ctx_len.numel() != S or new_tok.numel() != S:
         raise ValueError("ctx, ctx_len and new_tok disagree on S")
-    dev = ctx.device
-    _mx4_arg(rows, "rows", dev)
-    out_type = _float_type(out.dtype, "out")
+    _mx4_arg(rows, "rows", ctx.device)
+    code = _float_type(out.dtype, "out")
     if not out.is_contiguous() or out.numel() != S * rows.cols:
         raise ValueError("out must be contiguous with S * cols elements")
-    if ctx_len.device != dev or new_tok.device != dev or out.device != dev:
-        raise ValueError(f"ctx_len, new_tok and out must be on {dev}")
+    index = ctx.get_device()
+    if not index == ctx_len.get_device() == new_tok.get_device() == out.get_device():
+        raise ValueError(f"ctx_len, new_tok and out must be on {ctx.device}")
     for name, t, dt in (("fgram_ids", fgram_ids, torch.int32), ("match_len", match_len, torch.int8)):
         if t is not None and (t.dtype != dt or t.numel() != S or not t.is_contiguous()
-                              or t.device != dev):
-            raise ValueError(f"{name} must be a contiguous {dt} tensor of S elements on {dev}")
-    with _on(dev):
-        rc = lib().scone_decode_step_mx4(table.handle, _ptr(ctx), _ptr(ctx_len), cap,
-                                         _ptr(new_tok), S, int(max_n), rows.ptr, rows.n_rows,
-                                         rows.cols, rows.placement, _ptr(out), out_type,
-                                         _ptr(fgram_ids), _ptr(match_len), _stream(stream))
-    _check(rc, "scone_decode_step_mx4")
+                              or t.device != ctx.device):
+            raise ValueError(f"{name} must be a contiguous {dt} tensor of S elements on {ctx.device}")
+    _run("scone_decode_step_mx4", index, stream, lib().scone_decode_step_mx4, table.handle,
+         _ptr(ctx), ctx_len.data_ptr(), cap, new_tok.data_ptr(), S, int(max_n), rows.ptr,
+         rows.n_rows, rows.cols, rows.placement, out.data_ptr(), code, _ptr(fgram_ids),
+         _ptr(match_len))
     return out
 
 
@@ -869,75 +887,62 @@ def linear_mx4(x, w: Mx4Rows, bias: Optional[torch.Tensor] = None, gelu: bool = 
     `workspace` (a CUDA uint8 tensor of linear_mx4_workspace_bytes) or, when None, a
     tensor from torch's caching allocator."""
     _mx4_arg(w, "w")
-    if w.placement != PLACE_HBM:
-        raise ValueError("w must be device rows")
     dev, N, K = w.device, w.n_rows, w.cols
+    if dev is None:
+        raise ValueError("w must be device rows")
     if isinstance(x, Mx4Rows):
-        _mx4_arg(x, "x", dev)
-        if x.placement != PLACE_HBM:
+        if x.device is None:
             raise ValueError("x must be device rows")
-        M, Kx, lead, x_type, ld_x, x_ptr = x.n_rows, x.cols, (x.n_rows,), MX4, 0, x.ptr
-        dtype = torch.bfloat16 if dtype is None else dtype
+        x_type, M, Kx, ld_x, x_ptr, lead = MX4, x.n_rows, x.cols, 0, x.ptr, (x.n_rows,)
+        if dtype is None:
+            dtype = torch.bfloat16
     else:
-        if not isinstance(x, torch.Tensor) or not x.is_cuda:
-            raise TypeError("x must be a CUDA (HIP) tensor or Mx4Rows")
-        if x.dim() < 1:
-            raise ValueError("x must have at least one dimension")
-        lead, Kx = tuple(x.shape[:-1]), x.shape[-1]
-        if x.dim() != 2 and not x.is_contiguous():
-            raise ValueError("x must be contiguous, or a matrix with contiguous rows")
-        x2 = x if x.dim() == 2 else x.view(math.prod(lead), Kx)
-        ld_x = _float_matrix(x2, "x")
-        M, x_type, x_ptr = x2.shape[0], _TYPES[x.dtype], _ptr(x2)
-        dtype = x.dtype if dtype is None else dtype
-        if x.device != dev:
-            raise ValueError(f"x must be on {dev}")
+        x_type, M, Kx, ld_x = _float_rows(x, "x")
+        x_ptr, lead = x.data_ptr(), x.shape[:-1]
+        if dtype is None:
+            dtype = x.dtype
+    if x.device != dev:
+        raise ValueError(f"x must be on {dev}")
     if Kx != K:
         raise ValueError(f"x has rows of {Kx} elements, w of {K}")
+    shape = (*lead, N)
     if out is None:
-        _float_type(dtype, "dtype")
-        out = torch.empty(lead + (N,), dtype=dtype, device=dev)
-    if out.device != dev or tuple(out.shape) != lead + (N,):
-        raise ValueError(f"out must be [..., {N}] on {dev}")
-    out_type = _float_type(out.dtype, "out")
-    ld_out = _row_stride(out, M, N, "out")
+        out_type, ld_out = _float_type(dtype, "dtype"), N
+        out = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        out_type, _, _, ld_out = _float_rows(out, "out")
+        if out.device != dev or tuple(out.shape) != shape:
+            raise ValueError(f"out must be [..., {N}] on {dev}")
+        ld_out = ld_out if M > 1 else N
     if residual is not None:
         if residual.dtype != out.dtype or residual.shape != out.shape or residual.device != dev:
             raise ValueError("residual must have the result's shape, type and device")
-        if M > 1 and N > 0 and _row_stride(residual, M, N, "residual") != ld_out:
+        if _float_rows(residual, "residual")[3] != ld_out and M > 1 and N > 0:
             raise ValueError("residual must have the result's row stride")
-        _row_stride(residual, M, N, "residual")
-    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.device != dev
-                             or tuple(bias.shape) != (N,) or not bias.is_contiguous()):
-        raise ValueError(f"bias must be a contiguous tensor of {N} elements on {dev}")
-    bias_type = BF16 if bias is None else _float_type(bias.dtype, "bias")
-    with _on(dev):
-        need = lib().scone_linear_mx4_workspace(M, N, K, x_type)
-        if workspace is None:
-            if need > 0:
-                workspace = _scratch(need, dev, stream)
-                if workspace is None:
-                    raise SconeError(ENOMEM, "scone_linear_mx4")
-        elif workspace.dtype != torch.uint8 or workspace.device != dev \
-                or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
-        rc = lib().scone_linear_mx4(
-            x_ptr, x_type, ld_x, M, K, w.ptr, N, _ptr(bias), bias_type,
-            ACT_GELU if gelu else ACT_NONE, _ptr(residual), _ptr(out), out_type, ld_out,
-            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
-    _check(rc, "scone_linear_mx4")
+        residual = _ptr(residual)
+    bias_type = BF16
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor) or bias.device != dev \
+                or tuple(bias.shape) != (N,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous tensor of {N} elements on {dev}")
+        bias_type, bias = _float_type(bias.dtype, "bias"), _ptr(bias)
+    L, scratch = lib(), 0
+    if workspace is None:
+        need = L.scone_linear_mx4_workspace(M, N, K, x_type)
+        if need > 0:
+            workspace = _scratch(need, dev, stream)
+            if workspace is None:
+                raise SconeError(ENOMEM, "scone_linear_mx4")
+            scratch = need
+    elif workspace.dtype != torch.uint8 or workspace.device != dev \
+            or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+    else:
+        scratch = workspace.numel()
+    _run("scone_linear_mx4", out.get_device(), stream, L.scone_linear_mx4, x_ptr, x_type, ld_x, M,
+         K, w.ptr, N, bias, bias_type, ACT_GELU if gelu else ACT_NONE, residual, out.data_ptr(),
+         out_type, ld_out, _ptr(workspace), scratch)
     return out
-
-
-def _row_stride(t: torch.Tensor, M: int, N: int, name: str) -> int:
-    """The row stride of a result [..., N] of M rows: any for a matrix, N otherwise."""
-    if t.dim() == 2 and M > 1 and N > 0:
-        if (N > 1 and t.stride(1) != 1) or t.stride(0) < N:
-            raise ValueError(f"{name} must have contiguous rows that do not overlap")
-        return t.stride(0)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous, or a matrix with contiguous rows")
-    return N
 
 
 def check(stream=None, device=None) -> int:
