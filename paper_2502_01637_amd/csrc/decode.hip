@@ -193,7 +193,7 @@ hipError_t dispatch_slots(const scone_table* tb, int32_t* ctx, int32_t* ctx_len,
 }
 
 // The same step with the values of a 4-bit row (mx4.h) for the row: a lane takes
-// eight elements, the words and scale bytes of kMx4Pieces of them in flight.
+// 16 bytes of them at a time, the codes and scale bytes of kMx4Pieces in flight.
 constexpr int kMx4Pieces = 4;
 
 template <int SB, int G, int kType>
@@ -203,14 +203,14 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_mx4(
     const uint8_t* __restrict__ rows, int64_t n_rows, int cols,
     typename mx4::Elem<kType>::type* __restrict__ out, int32_t* __restrict__ ids_out,
     int8_t* __restrict__ len_out, unsigned* __restrict__ err, int64_t block0) {
-    typedef mx4::Elem<kType> E;
+    typedef mx4::Out<kType> O;
     const int64_t s = block_index(block0);
     const int lane = threadIdx.x;
     const int32_t rid = decode_find<SB, G>(slots, mask, ctx, ctx_len, ctx_cap, new_tok, max_n, s,
                                            lane, ids_out, len_out, err);
     const bool ok = (rid >= 0) & ((int64_t)rid < n_rows);
     if (!ok && lane == 0) atomicOr(err, err_bit(SCONE_EROW));
-    const int pieces = (cols + 7) / 8;
+    const int pieces = (cols + O::kElems - 1) / O::kElems;
     const uint8_t* row = rows + (ok ? rid : 0) * mx4::row_bytes(cols);
     const uint8_t* scales = row + 64 * mx4::groups(cols);
     auto* dst = out + s * cols;
@@ -221,8 +221,8 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_mx4(
             for (int u = 0; u < kMx4Pieces; ++u) {
                 const int c = c0 + u * kDecodeThreads;
                 if (c < pieces) {
-                    codes[u] = reinterpret_cast<const uint32_t*>(row)[c];
-                    sc[u] = scales[c >> 2];
+                    codes[u] = O::load(row, c);
+                    sc[u] = scales[c / (32 / O::kElems)];
                 }
             }
         }
@@ -230,8 +230,7 @@ __global__ __launch_bounds__(kDecodeThreads) void k_decode_mx4(
         for (int u = 0; u < kMx4Pieces; ++u) {
             const int c = c0 + u * kDecodeThreads;
             if (c < pieces)
-                mx4::store8<kType>(dst + c * 8, cols - c * 8,
-                                   E::values(codes[u], mx4::scale_of(sc[u])));
+                O::store(dst + c * O::kElems, cols - c * O::kElems, O::values(codes[u], sc[u]));
         }
     }
 }

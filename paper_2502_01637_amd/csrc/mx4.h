@@ -139,15 +139,6 @@ struct Elem<SCONE_FP32> {
         q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(v[6]), __uint_as_float(v[7]), scale, 3);
         return q;
     }
-    __device__ __forceinline__ static vec values(uint32_t q, float scale) {
-        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 0);
-        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 1);
-        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 2);
-        const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 3);
-        return vec{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x),
-                   __float_as_uint(b.y), __float_as_uint(c.x), __float_as_uint(c.y),
-                   __float_as_uint(d.x), __float_as_uint(d.y)};
-    }
 };
 
 // The scale byte of a block whose largest magnitude has this exponent field (that of
@@ -202,30 +193,43 @@ __device__ __forceinline__ typename Elem<kType>::vec load8(
     return v;
 }
 
-// The first n of eight elements to address p.
+// A lane's share of a row on its way out: 16 bytes, so that the lanes of a store cover
+// whole lines (two halves of 32 bytes of fp32, eight elements, took 450 us for the values
+// of 131,072 rows of 2,048 where pieces of four take 163).
 template <int kType>
-__device__ __forceinline__ void store8(typename Elem<kType>::type* p, int64_t n,
-                                       const typename Elem<kType>::vec& v) {
-    typedef typename Elem<kType>::vec vec;
-    if (n >= 8) {
-        if constexpr (sizeof(vec) == 16) {
+struct Out {
+    static constexpr int kElems = sizeof(typename Elem<kType>::type) == 4 ? 4 : 8;
+    // The piece's codes in their word (fp32: the low half of it).
+    __device__ __forceinline__ static uint32_t load(const uint8_t* row, int64_t c) {
+        if constexpr (kElems == 8) return reinterpret_cast<const uint32_t*>(row)[c];
+        else return reinterpret_cast<const uint16_t*>(row)[c];
+    }
+    __device__ __forceinline__ static u32x4 values(uint32_t q, uint32_t s) {
+        const float scale = scale_of(s);
+        if constexpr (kElems == 8) return Elem<kType>::values(q, scale);
+        else {
+            const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 0);
+            const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale, 1);
+            return u32x4{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x),
+                         __float_as_uint(b.y)};
+        }
+    }
+    // The first n elements of a piece to address p.
+    __device__ __forceinline__ static void store(typename Elem<kType>::type* p, int64_t n,
+                                                 const u32x4& v) {
+        if (n >= kElems) {
             __builtin_nontemporal_store(v, reinterpret_cast<u32x4_elem*>(p));
-        } else {
-            __builtin_nontemporal_store(u32x4{v[0], v[1], v[2], v[3]},
-                                        reinterpret_cast<u32x4_elem*>(p));
-            __builtin_nontemporal_store(u32x4{v[4], v[5], v[6], v[7]},
-                                        reinterpret_cast<u32x4_elem*>(p + 4));
+            return;
         }
-        return;
-    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i < n) {
-            if constexpr (sizeof(typename Elem<kType>::type) == 4) p[i] = v[i];
-            else p[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+        for (int i = 0; i < kElems; ++i) {
+            if (i < n) {
+                if constexpr (kElems == 4) p[i] = v[i];
+                else p[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            }
         }
     }
-}
+};
 
 // Quantise rows (the whole of scone_quantize_mx4 after its argument checks).
 hipError_t quantize(const void* x, int32_t type, int64_t n_rows, int64_t cols, int64_t ld,

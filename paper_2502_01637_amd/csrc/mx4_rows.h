@@ -1,9 +1,10 @@
 // Rows to 4 bits and back: quantisation, and the gather of 4-bit rows by id (mx4.h has
 // the format).
 //
-// Both are streams bound by memory: a lane takes eight elements (16 bytes of bf16 or
-// fp16, 32 of fp32, one word of codes), consecutive lanes consecutive pieces of a row, and
-// rows follow one another in a flat array of pieces, so that any width fills the lanes.
+// Both are streams bound by memory: a lane takes a piece of a row, consecutive lanes
+// consecutive pieces, and rows follow one another in a flat array of pieces, so that any
+// width fills the lanes.  On the way in a piece is eight elements (a word of codes), on
+// the way out 16 bytes.
 #pragma once
 
 #include "mx4.h"
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void k_gather_values(
     int64_t n_rows, int64_t cols, RowUnits pieces, int64_t row_bytes, int64_t scale_at,
     typename Elem<kType>::type* __restrict__ out, unsigned* __restrict__ err,
     int64_t block0) {
-    typedef Elem<kType> E;
+    typedef Out<kType> O;
     const int64_t base = block_index(block0) * (kThreads * U);
     const int64_t r0 = pieces.div64(base);
     const uint32_t c0 = (uint32_t)(base - r0 * pieces.upr);
@@ -98,18 +99,17 @@ __global__ __launch_bounds__(kThreads) void k_gather_values(
     for (int u = 0; u < U; ++u) {
         ok[u] = (id[u] >= 0) & (id[u] < n_rows);
         const uint8_t* row = rows + (ok[u] ? id[u] : 0) * row_bytes;
-        codes[u] = reinterpret_cast<const uint32_t*>(row)[c[u]];
-        s[u] = row[scale_at + (c[u] >> 2)];
+        codes[u] = O::load(row, c[u]);
+        s[u] = row[scale_at + c[u] / (32 / O::kElems)];
     }
     bool bad = false;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         bad |= in[u] & !ok[u];
         if (!in[u]) continue;
-        typename E::vec v = E::values(codes[u], scale_of(s[u]));
-        if (!ok[u]) v = typename E::vec{};
-        const int64_t e = (int64_t)c[u] * 8;
-        store8<kType>(out + r[u] * cols + e, cols - e, v);
+        const u32x4 v = ok[u] ? O::values(codes[u], s[u]) : u32x4{};
+        const int64_t e = (int64_t)c[u] * O::kElems;
+        O::store(out + r[u] * cols + e, cols - e, v);
     }
     if (bad) atomicOr(err, err_bit(SCONE_EROW));
 }
@@ -117,7 +117,8 @@ __global__ __launch_bounds__(kThreads) void k_gather_values(
 template <int kType, int U>
 hipError_t launch_gather(const int32_t* ids, int64_t n_tok, const void* rows, int64_t n_rows,
                              int64_t cols, void* out, unsigned* err, hipStream_t st) {
-    const RowUnits pieces = row_units((cols + 7) / 8, 1);
+    constexpr int E = Out<kType>::kElems;
+    const RowUnits pieces = row_units((cols + E - 1) / E, 1);
     const int64_t total = n_tok * pieces.upr;
     return launch_blocks((total + kThreads * U - 1) / (kThreads * U), kThreads,
                          [&](int64_t b0, dim3 grid) {
@@ -132,9 +133,9 @@ hipError_t launch_gather(const int32_t* ids, int64_t n_tok, const void* rows, in
 inline hipError_t gather(const int32_t* ids, int64_t n_tok, const void* rows, int64_t n_rows,
                          int64_t cols, void* out, int32_t type, unsigned* err, hipStream_t st) {
     switch (type) {
-        case SCONE_BF16: return launch_gather<SCONE_BF16, 4>(ids, n_tok, rows, n_rows, cols, out, err, st);
-        case SCONE_FP16: return launch_gather<SCONE_FP16, 4>(ids, n_tok, rows, n_rows, cols, out, err, st);
-        default: return launch_gather<SCONE_FP32, 4>(ids, n_tok, rows, n_rows, cols, out, err, st);
+        case SCONE_BF16: return launch_gather<SCONE_BF16, 2>(ids, n_tok, rows, n_rows, cols, out, err, st);
+        case SCONE_FP16: return launch_gather<SCONE_FP16, 2>(ids, n_tok, rows, n_rows, cols, out, err, st);
+        default: return launch_gather<SCONE_FP32, 2>(ids, n_tok, rows, n_rows, cols, out, err, st);
     }
 }
 
