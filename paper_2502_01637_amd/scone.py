@@ -883,7 +883,8 @@ def linear_mx4(x, w: Mx4Rows, bias: Optional[torch.Tensor] = None, gelu: bool = 
     or float32, quantised by the call) or 4-bit rows [M, K] (Mx4Rows), and w [N, K] in
     4 bits.  The result is [..., N] of `dtype` (default: x's, bfloat16 for 4-bit rows),
     or `out`, which may be a matrix with strided rows and may be the residual itself.
-    `residual` has the result's shape, type and row stride.  The scratch is
+    `residual` has the result's shape, type and row stride.  Results carry no gradient,
+    as everywhere in this module.  The scratch is
     `workspace` (a CUDA uint8 tensor of linear_mx4_workspace_bytes) or, when None, a
     tensor from torch's caching allocator."""
     _mx4_arg(w, "w")

@@ -5,7 +5,8 @@ exact, so where every product is a multiple of 2^-a and sum |x| |w| < 2^(24 - a)
 fp32 sum rounds, whatever its order, and results are equal to the bit; elsewhere each of
 the K additions is off by at most one unit of the last place (2^-23, rounded or cut) of
 a partial sum no larger than sum |x| |w|, the bias counted in.  GELU's polynomial is
-2.5e-7 off and its slope at most 1.13; each rounding to the output's type is off by half
+2.5e-7 off (for results of 16 bits 6.1e-6, or 4.4e-5 of its value) and its slope at most
+1.13; each rounding to the output's type is off by half
 a unit."""
 import numpy as np
 import pytest
@@ -266,13 +267,53 @@ def test_linear(M, N, K, x_type, out_type, bias_type, gelu, resid):
     S.linear_mx4(xin, S.Mx4Rows(dev(w), K), bias, gelu=gelu,
                  residual=out if resid == "in place" else res, out=out)
     got = f64(out)
-    tol = (K + 2) * 2.0 ** -23 * size * (1.13 if gelu else 1.0) + (3e-7 if gelu else 0.0)
+    tol = (K + 2) * 2.0 ** -23 * size * (1.13 if gelu else 1.0)
+    if gelu:
+        y = want if res is None else want - f64(res)
+        tol = tol + (3e-7 if out_type == torch.float32 else 6.1e-6 + 4.4e-5 * np.abs(y))
     if res is not None:
         tol = tol + 2.0 ** -24 * (np.abs(want) + np.abs(f64(res)))
     tol = tol + EPS[out_type] * (np.abs(want) + tol) + (2.0 ** -25 if out_type == torch.float16
                                                         else 0.0)
     assert (np.abs(got - want) <= tol).all(), np.max(np.abs(got - want) - tol)
     assert (buf[M] == 9.0).all() and (buf[:M, N:] == 9.0).all()
+
+
+# enough tiles of 128 x 256 for those, with ragged edges, over one to nine groups
+BIG = [(4100, 2100, 100), (4100, 2100, 200), (4096, 2048, 384), (2049, 4097, 512),
+       (4099, 2305, 640), (4100, 2100, 1100)]
+
+
+@pytest.mark.parametrize("M,N,K", BIG)
+def test_linear_big_tiles(M, N, K):
+    """To the bit without a residual; with one, a bias and GELU within the bounds."""
+    x, w = linear_case(M + K, M, N, K, True)
+    xq, wq = S.Mx4Rows(dev(x), K), S.Mx4Rows(dev(w), K)
+    xv = torch.from_numpy(mx4.values(x, K)).cuda()
+    wv = torch.from_numpy(mx4.values(w, K)).cuda()
+    want, size = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    assert float(size.max()) < 2 ** 20
+    assert torch.equal(S.linear_mx4(xq, wq, dtype=torch.float32).double(), want)
+    for dtype in TYPES:
+        bias, res = rng_tensor(N, (N,), dtype), rng_tensor(K, (M, N), dtype, 50.0)
+        # weights 1/64 as large: GELU where it bends
+        small = S.Mx4Rows(wq.data.clone(), K)
+        small.data[:, 64 * (-(-K // 128)):64 * (-(-K // 128)) - (-K // 32)] -= 6
+        got = S.linear_mx4(xq, small, bias, gelu=True, residual=res, dtype=dtype)
+        b64 = bias.double()
+        pre = want / 64 + b64
+        y = 0.5 * pre * torch.special.erfc(-pre * 0.5 ** 0.5)
+        full = y + res.double()
+        # the sum with the bias rounds K times at most; GELU's polynomial for results of
+        # 16 bits is 6.1e-6 off, or 4.4e-5 of its value
+        tol = 1.13 * (K + 2) * 2.0 ** -23 * (size / 64 + b64.abs())
+        tol = tol + (3e-7 if dtype == torch.float32 else 6.1e-6 + 4.4e-5 * y.abs())
+        tol = tol + 2.0 ** -24 * (full.abs() + res.double().abs())
+        tol = tol + EPS[dtype] * (full.abs() + tol) + (2.0 ** -25 if dtype == torch.float16 else 0)
+        assert ((got.double() - full).abs() <= tol).all(), dtype
+        inplace = res.clone()
+        S.linear_mx4(xq, small, bias, gelu=True, residual=inplace, out=inplace)
+        assert torch.equal(inplace, got)
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 40, 300), (16, 64, 1024), (70, 90, 500), (300, 300, 640)])
