@@ -453,6 +453,8 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(Slabs 
     // The sums begin with the biases; acc[i][m][r] is out[row m * 32 + lane % 32,
     // n i * 32 + 8 (r / 4) + 4 (lane / 32) + r % 4] of the wavefront's part.
     const int fr = lane & 31, half = lane >> 5;
+    // Three slabs in flight (the last again where there are fewer).
+    issue(0, 0);
     f32x4 bias[TN][4];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
@@ -460,8 +462,6 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(Slabs 
         for (int q = 0; q < 4; ++q)
             bias[i][q] = *reinterpret_cast<const f32x4*>(w.bias + n0 + (wn * TN + i) * 32 + q * 8 +
                                                          half * 4);
-    // Three slabs in flight (the last again where there are fewer).
-    issue(0, 0);
     issue(g > 1 ? 1 : 0, 1);
     issue(g > 2 ? 2 : g - 1, 2);
     f32x16 acc[TN][TM];
@@ -617,52 +617,66 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(Slabs 
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     uint8_t* const part = smem + wave * 32 * PITCH;
-    uint8_t* po = static_cast<uint8_t*>(ep.out) + at0 * kSize;
+    // kInside, kGelu: known (0, 1) or looked up (2).  Known, the way out is straight code
+    // that reads the next sums while others leave (280 -> 269 us for 65,459 x 4,096 x
+    // 1,024 with GELU).  With residuals that was slower (196 -> 216 us, x 1,024 x 4,096):
+    // more of them in flight hold up the copies of the other workgroup.
+    auto leave = [&](auto inside_c, auto gelu_c) {
+        constexpr int kInside = decltype(inside_c)::value, kGelu = decltype(gelu_c)::value;
+        uint8_t* po = static_cast<uint8_t*>(ep.out) + at0 * kSize;
 #pragma unroll
-    for (int batch = 0; batch < NB; ++batch) {
-        constexpr int kPerRowSet = NB / TM;  // batches per 32 rows
-        if (batch % kPerRowSet == 0) {
-            const int m = batch / kPerRowSet;
+        for (int batch = 0; batch < NB; ++batch) {
+            constexpr int kPerRowSet = NB / TM;  // batches per 32 rows
+            if (batch % kPerRowSet == 0) {
+                const int m = batch / kPerRowSet;
 #pragma unroll
-            for (int i = 0; i < TN; ++i)
+                for (int i = 0; i < TN; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<f32x4*>(part + fr * PITCH + (i * 32 + q * 8 + half * 4) * 4) =
-                        f32x4{acc[i][m][q * 4], acc[i][m][q * 4 + 1], acc[i][m][q * 4 + 2],
-                              acc[i][m][q * 4 + 3]};
-        }
-        if (batch + 1 < NB) load_residuals(batch + 1, res[(batch + 1) & 1]);
-#pragma unroll
-        for (int u = 0; u < NI; ++u, po += RPI * ep.ld * kSize) {
-            const int r = (batch % kPerRowSet * NI + u) * RPI + er;
-            float v[V];
-#pragma unroll
-            for (int e = 0; e < V; e += 4) {
-                const f32x4 s = *reinterpret_cast<const f32x4*>(part + r * PITCH + (ec + e) * 4);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[e + k] = s[k];
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<f32x4*>(part + fr * PITCH + (i * 32 + q * 8 + half * 4) * 4) =
+                            f32x4{acc[i][m][q * 4], acc[i][m][q * 4 + 1], acc[i][m][q * 4 + 2],
+                                  acc[i][m][q * 4 + 3]};
             }
-            if (ep.gelu)
+            if (batch + 1 < NB) load_residuals(batch + 1, res[(batch + 1) & 1]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = gelu_for<kOut>(v[e]);
-            if constexpr (kResid) {
-                float f[V];
-                widen<kOut>(res[batch & 1][u], f);
+            for (int u = 0; u < NI; ++u, po += RPI * ep.ld * kSize) {
+                const int r = (batch % kPerRowSet * NI + u) * RPI + er;
+                float v[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] += f[e];
-            }
-            const u32x4 o = narrow<kOut>(v);
-            if (inside) {
-                __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(po));
-            } else if ((batch * NI + u) * RPI < rows) {
+                for (int e = 0; e < V; e += 4) {
+                    const f32x4 s = *reinterpret_cast<const f32x4*>(part + r * PITCH + (ec + e) * 4);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (e >= left) continue;
-                    if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(po)[e] = o[e];
-                    else reinterpret_cast<uint16_t*>(po)[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+                    for (int k = 0; k < 4; ++k) v[e + k] = s[k];
+                }
+                if (kGelu == 2 ? ep.gelu : kGelu == 1)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = gelu_for<kOut>(v[e]);
+                if constexpr (kResid) {
+                    float f[V];
+                    widen<kOut>(res[batch & 1][u], f);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] += f[e];
+                }
+                const u32x4 o = narrow<kOut>(v);
+                if (kInside == 2 ? inside : kInside == 1) {
+                    __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(po));
+                } else if ((batch * NI + u) * RPI < rows) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        if (e >= left) continue;
+                        if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(po)[e] = o[e];
+                        else reinterpret_cast<uint16_t*>(po)[e] = (uint16_t)(o[e / 2] >> (16 * (e & 1)));
+                    }
                 }
             }
         }
+    };
+    if constexpr (kResid) {
+        leave(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+    } else {
+        if (!inside) leave(integral_constant<int, 0>{}, integral_constant<int, 2>{});
+        else if (ep.gelu) leave(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+        else leave(integral_constant<int, 1>{}, integral_constant<int, 0>{});
     }
 }
 
