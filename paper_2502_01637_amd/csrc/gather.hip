@@ -285,5 +285,6 @@ extern "C" int scone_gather_mx4(const int32_t* fgram_ids, int64_t n_tok, const v
     if (!err) return SCONE_EHIP;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (n_rows == 0) return status_of(launch_zero_rows(out, out_b, err, st));
-    return status_of(mx4::gather(fgram_ids, n_tok, rows, n_rows, cols, out, out_type, err, st));
+    return status_of(mx4::gather(fgram_ids, n_tok, rows, n_rows, cols, out, out_type,
+                                 placement, err, st));
 }
