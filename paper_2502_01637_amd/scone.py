@@ -694,7 +694,7 @@ def gather_split(fgram_ids: torch.Tensor, near_rows: torch.Tensor, far_rows: "Ho
 _TYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 
 
-@functools.lru_cache(maxsize=None)
+@functools.lru_cache(maxsize=1024)
 def mx4_row_bytes(cols: int) -> int:
     """Bytes of a 4-bit row of `cols` elements (scone_mx4_row_bytes)."""
     n = int(lib().scone_mx4_row_bytes(int(cols)))
@@ -711,7 +711,7 @@ class Mx4Rows:
     HostRows of such rows in pinned host memory (``device`` is then None).  The calls
     that move rows as bytes (gather, embed, gather_split, ...) take ``data``."""
 
-    __slots__ = ("data", "cols", "row_bytes", "placement", "n_rows", "device", "ptr")
+    __slots__ = ("data", "cols", "row_bytes", "placement", "n_rows", "device")
 
     def __init__(self, data, cols: int):
         row_bytes = mx4_row_bytes(int(cols))
@@ -721,7 +721,7 @@ class Mx4Rows:
         if ptr is not None and ptr % 16:
             raise ValueError("data must be 16-byte aligned")
         self.data, self.cols, self.row_bytes = data, int(cols), row_bytes
-        self.placement, self.n_rows, self.ptr = placement, n_rows, ptr
+        self.placement, self.n_rows = placement, n_rows
         self.device = data.device if placement == PLACE_HBM else None
 
     @classmethod
@@ -733,6 +733,17 @@ class Mx4Rows:
     @property
     def nbytes(self) -> int:
         return self.n_rows * self.row_bytes
+
+    @property
+    def ptr(self):
+        """Address of the rows (None where there are none).  A tensor that has been
+        resized since is refused."""
+        data = self.data
+        if self.placement == PLACE_HOST:
+            return data.device_ptr
+        if data.numel() != self.n_rows * self.row_bytes:
+            raise ValueError("the tensor of 4-bit rows has changed its size")
+        return data.data_ptr() or None
 
 
 def _mx4_arg(rows, name: str, device: Optional[torch.device] = None):

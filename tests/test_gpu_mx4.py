@@ -343,6 +343,18 @@ def test_linear_scales_at_the_ends():
         assert np.array_equal(got, mx4.values(x, K) @ mx4.values(w, K).T)
 
 
+@pytest.mark.parametrize("M", [3, 70])
+def test_linear_products_past_the_range(M):
+    """Products past fp32's range are infinities of their sign; codes of 0 stay 0 under
+    the largest scales.  Codes are 6 and 0, so that 36 x 2^250 is a product's size."""
+    x = torch.zeros((M, 200), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((5, 200), dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 3e38
+    w[0, 0], w[1, 1], w[2, 0], w[3, 130], w[4, 0] = 3e38, 3e38, -3e38, 3e38, 2.0 ** -100
+    got = f64(S.linear_mx4(x, S.quantize_mx4(w), dtype=torch.float32))
+    assert np.array_equal(got, np.tile([np.inf, 0, -np.inf, 0, 6 * 2.0 ** 25], (M, 1)))
+
+
 def test_linear_empty_sizes():
     w = S.Mx4Rows(dev(packed(1, 8, 100)), 100)
     none = S.Mx4Rows(torch.empty((0, 80), dtype=torch.uint8, device="cuda"), 100)
@@ -367,6 +379,17 @@ def test_linear_far_output():
 
 
 # --------------------------------------------- refusals, streams and graphs ----
+
+def test_a_resized_tensor_of_rows_is_refused():
+    rows = S.quantize_mx4(rng_tensor(2, (6, 100), torch.bfloat16))
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    S.gather_mx4(ids, rows)
+    rows.data.resize_((2, rows.row_bytes))
+    for call in (lambda: S.gather_mx4(ids, rows), lambda: S.dequantize_mx4(rows),
+                 lambda: S.linear_mx4(rng_tensor(1, (4, 100), torch.bfloat16), rows)):
+        with pytest.raises(ValueError):
+            call()
+
 
 def test_binding_refuses_mismatches():
     x = rng_tensor(1, (4, 100), torch.bfloat16)
