@@ -399,9 +399,8 @@ constexpr int workgroups(int tm, int tn) {
 // ring, and leave it by whole rows: a lane takes four consecutive n, adds the bias, and
 // rounds once behind activation and residual.
 template <int TM, int TN, int kOut, bool kResid>
-__global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(Slabs x, Slabs w, int g, Epilogue ep,
-                                                         uint32_t tiles_m, uint32_t tiles_n,
-                                                         int64_t block0) {
+__global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
+    Slabs x, Slabs w, int g, Epilogue ep, uint32_t tiles_m, uint32_t tiles_n, int64_t block0) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
     constexpr int SX = (BM + BN) * 64, SW = SX + 1024;  // the scales behind the codes
     constexpr int STAGE = stage_bytes(TM, TN);
@@ -714,9 +713,9 @@ inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const 
 // Whether a product takes the tiles.  k_linear_few quantises x again in every workgroup,
 // so from 17 rows on it pays as long as that is little: blocks of 16 rows of x by groups,
 // up to 64 in a workgroup and 8,192 in all.  Against the tiles, us, at 16, 32 and 64 rows:
-// N 4,096, K 1,024 3.8, 5.0, 7.1 and 8.5, 9.0, 8.7; 4,001 x 1,500 4.9, 6.8, 10.7 and 9.8,
-// 10.4, 10.4; 1,024 x 4,096 7.7, 11.2, 18.6 and 13.5, 14.1, 13.5; 16,384 x 4,096 23.7,
-// 38.1, 66.7 and 25.4, 25.9, 25.2.
+// N 4,096, K 1,024 3.7, 4.6, 6.9 and 8.3, 8.9, 8.5; 4,001 x 1,500 6.3, 8.7, 11.1 and 9.8,
+// 10.4, 10.5; 1,024 x 4,096 6.9, 10.1, 17.1 and 13.5, 14.0, 13.3; 16,384 x 4,096 19.4,
+// 27.9, 49.9 and 25.3, 25.7, 25.0.
 inline bool tiled(int64_t M, int64_t N, int64_t K) {
     if (M <= 16) return false;
     const int64_t blocks = (M <= 32 ? 2 : 4) * groups(K);
@@ -758,8 +757,14 @@ inline hipError_t linear(const void* x, int32_t type, int64_t ld, const uint8_t*
         default: e = launch_slabs<SCONE_MX4>(x, ld, sx, w, sw, K, ep, st);
     }
     if (e != hipSuccess) return e;
+    // The large tiles from one a compute unit on, the small ones below, of which there
+    // are four times as many.  Us, large and small, at 96, 192, 256, 512 and 1,024 large
+    // tiles: N 4,096, K 1,024 12.2, 14.0, 15.4, 23.0, 34.9 and 11.8, 14.1, 15.9, 24.1, 39.1;
+    // N 16,384, K 4,096 (from 128 on) 31.8, 33.2, 36.6, 53.1, 86.6 and 30.0, 36.5, 41.8,
+    // 65.6, 115.
     const int64_t big = ((ep.M + 127) / 128) * ((ep.N + 255) / 256);
-        return big >= 256 ? launch_tiles<2, 4>(sx, sw, K, ep, st) : launch_tiles<1, 2>(sx, sw, K, ep, st);
+    return big >= 256 ? launch_tiles<2, 4>(sx, sw, K, ep, st)
+                      : launch_tiles<1, 2>(sx, sw, K, ep, st);
 }
 
 }  // namespace mx4
