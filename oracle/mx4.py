@@ -1,4 +1,4 @@
-"""Microscaled 4-bit rows in plain numpy, 64 bits (the checker of the 4-bit calls).
+"""Microscaled 4-bit rows in plain numpy, 64 bits (the oracle of the 4-bit calls).
 
 From the definition (OCP Microscaling Formats v1.0: E2M1 elements, E8M0 scales,
 blocks of 32) and the row layout that include/scone.h states.
