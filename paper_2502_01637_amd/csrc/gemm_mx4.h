@@ -398,7 +398,12 @@ constexpr int workgroups(int tm, int tn) {
 // Results go through LDS as fp32, 32 rows at a time in each wavefront's own part of the
 // ring, and leave it by whole rows: a lane takes four consecutive n, adds the bias, and
 // rounds once behind activation and residual.
-template <int TM, int TN, int kOut, bool kResid>
+//
+// kLines: results pass by the caches.  So where rows are whole runs of 64 bytes;
+// elsewhere the caches join what two workgroups write of one (36,827 x 2,507 x 804 to
+// fp32 142 us past them, 127 through; x 2,544, 159 runs, 100 and 110; x 2,560 95 and 106;
+// where all of the results fit the caches the two are within 5 % of each other).
+template <int TM, int TN, int kOut, bool kResid, bool kLines>
 __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
     Slabs x, Slabs w, int g, Epilogue ep, uint32_t tiles_m, uint32_t tiles_n, int64_t block0) {
     constexpr int BM = 64 * TM, BN = 64 * TN;
@@ -626,6 +631,10 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
     // more of them in flight hold up the copies of the other workgroup.
     // In tiles over an edge the lanes whose columns are all there still move 16 bytes
     // (by elements 1,000 x 16,384 x 4,096 took 58.7 us, now 50.2).
+    auto store = [&](const u32x4& o, uint8_t* to) {
+        if constexpr (kLines) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(to));
+        else *reinterpret_cast<u32x4_out*>(to) = o;
+    };
     auto leave = [&](auto inside_c, auto gelu_c) {
         constexpr int kInside = decltype(inside_c)::value, kGelu = decltype(gelu_c)::value;
         uint8_t* po = static_cast<uint8_t*>(ep.out) + at0 * kSize;
@@ -664,10 +673,10 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
                 }
                 const u32x4 o = narrow<kOut>(v);
                 if (kInside == 2 ? inside : kInside == 1) {
-                    __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(po));
+                    store(o, po);
                 } else if ((batch * NI + u) * RPI < rows) {
                     if (left == V) {
-                        __builtin_nontemporal_store(o, reinterpret_cast<u32x4_out*>(po));
+                        store(o, po);
                         continue;
                     }
 #pragma unroll
@@ -689,7 +698,7 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
     }
 }
 
-template <int TM, int TN, int kOut, bool kResid>
+template <int TM, int TN, int kOut, bool kResid, bool kLines>
 inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
                                hipStream_t st) {
     const int64_t tiles_m = (ep.M + 64 * TM - 1) / (64 * TM);
@@ -697,26 +706,35 @@ inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const 
     // the kernel counts tiles in 32 bits (2^28 of them hold a terabyte of results)
     if (tiles_m * tiles_n > ((int64_t)1 << 28)) return hipErrorInvalidConfiguration;
     return launch_blocks(tiles_m * tiles_n, 256, [&](int64_t b0, dim3 grid) {
-        hipLaunchKernelGGL((k_linear_tiles<TM, TN, kOut, kResid>), grid, dim3(256), 0, st, x,
+        hipLaunchKernelGGL((k_linear_tiles<TM, TN, kOut, kResid, kLines>), grid, dim3(256), 0, st, x,
                            w, (int)groups(K), ep, (uint32_t)tiles_m,
                            (uint32_t)tiles_n, b0);
     });
 }
 
+template <int TM, int TN, int kOut, bool kResid>
+inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
+                               hipStream_t st) {
+    const uintptr_t row = (uintptr_t)ep.ld * (16 / kPer16<kOut>);
+    return ((uintptr_t)ep.out | row) % 64 == 0
+               ? launch_tiles<TM, TN, kOut, kResid, true>(x, w, K, ep, st)
+               : launch_tiles<TM, TN, kOut, kResid, false>(x, w, K, ep, st);
+}
+
+template <int TM, int TN, int kOut>
+inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
+                               hipStream_t st) {
+    return ep.residual ? launch_tiles<TM, TN, kOut, true>(x, w, K, ep, st)
+                       : launch_tiles<TM, TN, kOut, false>(x, w, K, ep, st);
+}
+
 template <int TM, int TN>
 inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const Epilogue& ep,
                                hipStream_t st) {
-    const bool r = ep.residual != nullptr;
     switch (ep.out_type) {
-        case SCONE_BF16:
-            return r ? launch_tiles<TM, TN, SCONE_BF16, true>(x, w, K, ep, st)
-                     : launch_tiles<TM, TN, SCONE_BF16, false>(x, w, K, ep, st);
-        case SCONE_FP16:
-            return r ? launch_tiles<TM, TN, SCONE_FP16, true>(x, w, K, ep, st)
-                     : launch_tiles<TM, TN, SCONE_FP16, false>(x, w, K, ep, st);
-        default:
-            return r ? launch_tiles<TM, TN, SCONE_FP32, true>(x, w, K, ep, st)
-                     : launch_tiles<TM, TN, SCONE_FP32, false>(x, w, K, ep, st);
+        case SCONE_BF16: return launch_tiles<TM, TN, SCONE_BF16>(x, w, K, ep, st);
+        case SCONE_FP16: return launch_tiles<TM, TN, SCONE_FP16>(x, w, K, ep, st);
+        default: return launch_tiles<TM, TN, SCONE_FP32>(x, w, K, ep, st);
     }
 }
 
