@@ -85,28 +85,6 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
     return v;
 }
 
-// GELU for results that are rounded to 16 bits: gemm::gelu_erf's form with a polynomial
-// of degree 5 on [0, 5.5] (closest in the largest relative error, weighted down beyond
-// 3).  Within 4.4e-5 of the value down to x = -3 and 6.1e-6 of it anywhere, where the
-// rounding is 2^-9 (bf16) or 2^-11 (fp16): a product whose results were GELUs of
-// degree 9 spent as long on them as on its sums.
-__device__ __forceinline__ float gelu_16(float x) {
-    const float z = __builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.0f, 5.5f);
-    float p = -3.74266548e-04f;
-    p = p * z + 6.33217741e-03f;
-    p = p * z - 4.98651324e-02f;
-    p = p * z - 4.62025925e-01f;
-    p = p * z - 1.15009108f;
-    p = p * z - 1.00006211f;
-    const float pos = __builtin_fmaf(0.5f, __builtin_fabsf(x), 0.5f * x);
-    return pos - z * __builtin_amdgcn_exp2f(p);
-}
-
-template <int kOut>
-__device__ __forceinline__ float gelu_for(float x) {
-    return kOut == SCONE_FP32 ? gemm::gelu_erf(x) : gelu_16(x);
-}
-
 // Few rows of x: the weights are read once, from memory straight into the lanes, and
 // bound the time.  A workgroup of kFewWaves wavefronts takes 16 rows of w; a round is
 // kFewWaves groups, one a wavefront, whose weights are on their way kFewAhead rounds
@@ -251,7 +229,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __res
 #pragma unroll
         for (int j = 0; j < kFewWaves; ++j) v += sums[j * kRows * 16 + t];
         if (ep.bias) v += load_elem(ep.bias, ep.bias_type, n);
-        if (ep.gelu) v = ep.out_type == SCONE_FP32 ? gemm::gelu_erf(v) : gelu_16(v);
+        if (ep.gelu) v = gemm::gelu_erf(v);
         if (ep.residual) v += load_elem(ep.residual, ep.out_type, row * ep.ld + n);
         store_elem(ep.out, ep.out_type, row * ep.ld + n, v);
     }
@@ -664,7 +642,7 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
                 }
                 if (kGelu == 2 ? ep.gelu : kGelu == 1)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] = gelu_for<kOut>(v[e]);
+                    for (int e = 0; e < V; ++e) v[e] = gemm::gelu_erf(v[e]);
                 if constexpr (kResid) {
                     float f[V];
                     widen<kOut>(res[batch & 1][u], f);
