@@ -73,6 +73,9 @@ __device__ __forceinline__ void widen(const u32x4& v, float (&f)[kPer16<kType>])
     }
 }
 
+// The values are fp32 before they are rounded: without the empty asm the compiler joins
+// a multiply-add that computes one with its rounding to fp16 (v_fma_mix) where no branch
+// lies between, and a value's last bit went by the tile that it lay in.
 template <int kType>
 __device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
     u32x4 v;
@@ -80,7 +83,11 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
     for (int i = 0; i < 4; ++i) {
         if constexpr (kType == SCONE_FP32) v[i] = __float_as_uint(f[i]);
         else if constexpr (kType == SCONE_BF16) v[i] = gemm::pack_bf16x2(f[2 * i], f[2 * i + 1]);
-        else v[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)f[2 * i], (_Float16)f[2 * i + 1]});
+        else {
+            float a = f[2 * i], b = f[2 * i + 1];
+            asm("" : "+v"(a), "+v"(b));
+            v[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+        }
     }
     return v;
 }

@@ -58,3 +58,18 @@ def test_gelu_of_infinities_and_nan(M, dtype):
     assert (got[:, 3] == float("inf")).all() and torch.isnan(got[:, [700, 4095]]).all()
     got[:, [3, 700, 4095]] = 0
     assert not got.any()
+
+
+@pytest.mark.parametrize("M,N", [(100, 1024), (1100, 8191)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_a_value_does_not_depend_on_its_tile(M, N, dtype):
+    """Equal rows give equal results in whole tiles and in tiles over an edge, and their
+    16-bit results are the fp32 ones rounded to nearest."""
+    K = 64
+    w = S.quantize_mx4(torch.zeros((N, K), dtype=torch.bfloat16, device="cuda"))
+    x = torch.zeros((M, K), device="cuda")
+    for lo, hi in [(-8.0, 0.0), (0.0, 8.0)]:
+        b = torch.linspace(lo, hi, N, dtype=torch.float64).float().cuda()
+        got = S.linear_mx4(x, w, b, gelu=True, dtype=dtype)
+        assert torch.equal(got, S.linear_mx4(x, w, b, gelu=True, dtype=torch.float32).to(dtype))
+        assert torch.equal(got, got[:1].expand(M, N))
