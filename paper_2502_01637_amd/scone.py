@@ -183,12 +183,31 @@ def _scratch(nbytes: int, device: torch.device, stream) -> Optional[torch.Tensor
     try:
         if stream is None:
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(_stream(stream), device=device)
-        with torch.cuda.stream(stream):
+        with torch.cuda.stream(_torch_stream(stream, device)):
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
     except torch.OutOfMemoryError:
         return None
+
+
+def _torch_stream(stream, device: torch.device):
+    """`stream` (a torch stream, another object that has its handle, or the handle)
+    as a torch stream."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(_stream(stream), device=device)
+
+
+def _result(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
+    """Memory for a call's result, ordered on the stream that the call runs on as
+    _scratch is: another stream's work may still use a block that it gave back, and this
+    one's a result that is dropped.  The current stream is where the program uses the
+    result (once it waits for `stream`), so the memory waits for it too."""
+    if stream is None or _stream(stream) == _raw_stream(device.index):
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(torch.cuda.current_stream(device))
+    return out
 
 
 def _dev_i32(t: torch.Tensor, name: str, ndim: Optional[int] = None) -> torch.Tensor:
@@ -800,7 +819,7 @@ def quantize_mx4(x: torch.Tensor, out: Optional[Mx4Rows] = None, stream=None) ->
     row stride) in 4 bits."""
     code, n, cols, ld = _float_rows(x, "x", 2)
     if out is None:
-        out = Mx4Rows.empty(n, cols, x.device)
+        out = Mx4Rows(_result((n, mx4_row_bytes(cols)), torch.uint8, x.device, stream), cols)
     else:
         _mx4_arg(out, "out", x.device)
         if out.placement != PLACE_HBM or out.n_rows != n or out.cols != cols:
@@ -833,7 +852,7 @@ def _gather_mx4(ids, shape, device, rows, dtype, out, stream):
     cols = rows.cols
     if out is None:
         code = _float_type(dtype, "dtype")
-        out = torch.empty((*shape, cols), dtype=dtype, device=device)
+        out = _result((*shape, cols), dtype, device, stream)
         n_tok = math.prod(shape)
     else:
         code = _float_type(out.dtype, "out")
@@ -920,7 +939,7 @@ def linear_mx4(x, w: Mx4Rows, bias: Optional[torch.Tensor] = None, gelu: bool = 
     shape = (*lead, N)
     if out is None:
         out_type, ld_out = _float_type(dtype, "dtype"), N
-        out = torch.empty(shape, dtype=dtype, device=dev)
+        out = _result(shape, dtype, dev, stream)
     else:
         out_type, _, _, ld_out = _float_rows(out, "out")
         if out.device != dev or tuple(out.shape) != shape:
