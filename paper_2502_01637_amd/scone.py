@@ -447,7 +447,8 @@ class FgramModel:
 class FgramModelMx4(FgramModel):
     """An f-gram model whose linear maps have 4-bit weights (scone_fgram_model_quantize),
     made from a FgramModel; its other parameters are shared with that model.
-    precompute_fgram_rows rounds the inputs of its products to 4 bits too.  Returns
+    precompute_fgram_rows rounds the inputs of its products to 4 bits too.  `stream`
+    waits for the current one, which may still copy the model's parameters.  Returns
     when the weights are written, so that any stream may use them."""
 
     def __init__(self, model: FgramModel, stream=None):
@@ -455,8 +456,10 @@ class FgramModelMx4(FgramModel):
         self.n_layers, self.max_len = model.n_layers, model.max_len
         self.blob, self.device = model.blob, model.blob.device
         n = lib().scone_fgram_model_mx4_bytes(self.d, self.n_heads, self.d_ff, self.n_layers)
-        self.weights = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        self.weights = _result((max(n, 16),), torch.uint8, self.device, stream)
         with _on(self.device):
+            if stream is not None:
+                _torch_stream(stream, self.device).wait_stream(torch.cuda.current_stream())
             rc = lib().scone_fgram_model_quantize(
                 self.blob.data_ptr(), self.d, self.n_heads, self.d_ff, self.n_layers,
                 self.max_len, self.weights.data_ptr(), _stream(stream))

@@ -88,3 +88,21 @@ def test_4bit_chain_captured_over_two_streams():
         torch.cuda.synchronize()
         assert torch.equal(got, want), seed
         np.testing.assert_equal(S.check(), S.scone.OK)
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_4bit_model_made_on_a_side_stream(as_handle):
+    """From parameters that the current stream is still copying."""
+    from workloads.fgram_model import ModelConfig, make_params
+    cfg = ModelConfig(512, 8, 1024, 2, 3)
+    P = {k: torch.from_numpy(np.array(v).view(np.int16)).cuda()
+         for k, v in make_params(cfg, seed=4).items()}
+    want = S.FgramModelMx4(S.FgramModel(P, 512, 8, 1024, 2, 3)).weights
+    side = torch.cuda.Stream()
+    busy = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        for k in range(20):
+            busy.fill_(k)
+        model = S.FgramModel(P, 512, 8, 1024, 2, 3)
+        four = S.FgramModelMx4(model, stream=side.cuda_stream if as_handle else side)
+        assert torch.equal(four.weights, want) and owner(four.weights) == side.cuda_stream

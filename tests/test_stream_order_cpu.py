@@ -130,3 +130,19 @@ def test_results_are_taken_on_the_launch_stream(gpu, call, kind):
     stream, handle = {"none": (None, 5), "current": (gpu.current, 5), "current handle": (5, 5),
                       "other": (Stream(8), 8), "other handle": (8, 8)}[kind]
     check(gpu, call, stream, handle)
+
+
+@pytest.mark.parametrize("stream", [Stream(8), 8], ids=["object", "handle"])
+def test_4bit_model_waits_for_the_model_it_is_made_from(gpu, stream):
+    """The parameters may still be on their way on the current stream."""
+    made = [stream] if isinstance(stream, Stream) else []
+    gpu.monkeypatch.setattr(torch.cuda, "ExternalStream",
+                            lambda *a, **k: made.append(Stream(*a, **k)) or made[-1])
+    model = types.SimpleNamespace(d=512, n_heads=8, d_ff=1024, n_layers=2, max_len=3,
+                                  blob=gpu.tensor(100, dtype=torch.int16))
+    four = S.FgramModelMx4(model, stream=stream)
+    assert gpu.launched == [("scone_fgram_model_quantize", 8)]
+    assert four.weights.on == 8 and four.weights.also == 5
+    assert [h for s in made for h in s.waits] == [5]
+    gpu.launched.clear()
+    assert S.FgramModelMx4(model).weights.on == 5 and gpu.launched[0][1] == 5
