@@ -305,12 +305,12 @@ def lookup(table: Table, token_ids: torch.Tensor, max_n: int,
     _dev_i32(token_ids, "token_ids", 2)
     B, T = token_ids.shape
     if fgram_ids is None:
-        fgram_ids = torch.empty((B, T), dtype=torch.int32, device=token_ids.device)
+        fgram_ids = _result((B, T), torch.int32, token_ids.device, stream)
     _dev_i32(fgram_ids, "fgram_ids")
     if fgram_ids.numel() != B * T:
         raise ValueError("fgram_ids has the wrong size")
     if match_len is None and want_len:
-        match_len = torch.empty((B, T), dtype=torch.int8, device=token_ids.device)
+        match_len = _result((B, T), torch.int8, token_ids.device, stream)
     if match_len is not None and (match_len.dtype != torch.int8 or match_len.numel() != B * T
                                   or not match_len.is_contiguous()):
         raise ValueError("match_len must be a contiguous int8 tensor of B*T elements")
@@ -327,15 +327,17 @@ def lookup_counted(table: Table, token_ids: torch.Tensor, max_n: int,
     probed).  Synchronises the stream to read the count."""
     _dev_i32(token_ids, "token_ids", 2)
     B, T = token_ids.shape
-    fgram_ids = torch.empty((B, T), dtype=torch.int32, device=token_ids.device)
-    match_len = torch.empty((B, T), dtype=torch.int8, device=token_ids.device)
-    probes = torch.zeros(1, dtype=torch.int64, device=token_ids.device)
-    with _on(token_ids.device):
+    dev = token_ids.device
+    fgram_ids = _result((B, T), torch.int32, dev, stream)
+    match_len = _result((B, T), torch.int8, dev, stream)
+    # the count is cleared, added to and read on one stream
+    with _on(dev), _HERE if stream is None else torch.cuda.stream(_torch_stream(stream, dev)):
+        probes = torch.zeros(1, dtype=torch.int64, device=dev)
         rc = lib().scone_lookup_counted(table.handle, _ptr(token_ids), B, T, int(max_n),
                                         _ptr(fgram_ids), _ptr(match_len), _ptr(probes),
                                         _stream(stream))
-    _check(rc, "scone_lookup_counted")
-    return fgram_ids, match_len, int(probes.item())
+        _check(rc, "scone_lookup_counted")
+        return fgram_ids, match_len, int(probes.item())
 
 
 def tag(table: Table, token_ids: torch.Tensor, max_n: int,
@@ -346,7 +348,7 @@ def tag(table: Table, token_ids: torch.Tensor, max_n: int,
     _dev_i32(token_ids, "token_ids", 2)
     B, T = token_ids.shape
     if match_len is None and want_len:
-        match_len = torch.empty((B, T), dtype=torch.int8, device=token_ids.device)
+        match_len = _result((B, T), torch.int8, token_ids.device, stream)
     if match_len is not None and (match_len.dtype != torch.int8 or match_len.numel() != B * T
                                   or not match_len.is_contiguous()):
         raise ValueError("match_len must be a contiguous int8 tensor of B*T elements")
@@ -378,13 +380,13 @@ def discover_fgrams(token_ids: torch.Tensor, max_len: int, S: int, min_count: in
     dev = token_ids.device
     need = discover_workspace_bytes(B, T, max_len)
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _result((need,), torch.uint8, dev, stream)
     if workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != dev
                                   or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor on the tokens' device")
-    fg = torch.empty((max(S, 1), max_len), dtype=torch.int32, device=dev)
-    ln = torch.empty(max(S, 1), dtype=torch.int32, device=dev)
-    ct = torch.empty(max(S, 1), dtype=torch.int32, device=dev)
+    fg = _result((max(S, 1), max_len), torch.int32, dev, stream)
+    ln = _result((max(S, 1),), torch.int32, dev, stream)
+    ct = _result((max(S, 1),), torch.int32, dev, stream)
     n = ctypes.c_int64()
     with _on(dev):
         rc = lib().scone_discover_fgrams(_ptr(token_ids), B, T, int(max_len), int(min_count),
@@ -561,8 +563,7 @@ def gather(fgram_ids: torch.Tensor, rows, out: Optional[torch.Tensor] = None,
     n_tok = fgram_ids.numel()
     placement, base, n_rows, row_bytes, row_shape, dtype = _rows_arg(rows)
     if out is None:
-        out = torch.empty(tuple(fgram_ids.shape) + row_shape, dtype=dtype,
-                          device=fgram_ids.device)
+        out = _result(tuple(fgram_ids.shape) + row_shape, dtype, fgram_ids.device, stream)
     if not out.is_contiguous() or out.numel() * out.element_size() != n_tok * row_bytes:
         raise ValueError("out must be contiguous with n_tok * row_bytes bytes")
     with _on(fgram_ids.device):
@@ -594,7 +595,7 @@ def embed(table: Table, token_ids: torch.Tensor, max_n: int, rows, out=None,
     B, T = token_ids.shape
     placement, base, n_rows, row_bytes, row_shape, dtype = _rows_arg(rows)
     if out is None:
-        out = torch.empty((B, T) + row_shape, dtype=dtype, device=token_ids.device)
+        out = _result((B, T) + row_shape, dtype, token_ids.device, stream)
     if not out.is_contiguous() or out.numel() * out.element_size() != B * T * row_bytes:
         raise ValueError("out must be contiguous with B * T * row_bytes bytes")
     for name, t, dt in (("fgram_ids", fgram_ids, torch.int32), ("match_len", match_len, torch.int8)):
@@ -634,8 +635,7 @@ def embed_pipelined(table: Table, next_tokens: Optional[torch.Tensor], max_n: in
         _dev_i32(cur_ids, "cur_ids")
         n_cur = cur_ids.numel()
         if out is None:
-            out = torch.empty(tuple(cur_ids.shape) + row_shape, dtype=dtype,
-                              device=cur_ids.device)
+            out = _result(tuple(cur_ids.shape) + row_shape, dtype, cur_ids.device, stream)
         if not out.is_contiguous() or out.numel() * out.element_size() != n_cur * row_bytes:
             raise ValueError("out must be contiguous with n_cur * row_bytes bytes")
     device = next_tokens.device if next_tokens is not None else (
@@ -697,7 +697,7 @@ def gather_split(fgram_ids: torch.Tensor, near_rows: torch.Tensor, far_rows: "Ho
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
     if out is None:
-        out = torch.empty(tuple(fgram_ids.shape) + shape_n, dtype=dt_n, device=fgram_ids.device)
+        out = _result(tuple(fgram_ids.shape) + shape_n, dt_n, fgram_ids.device, stream)
     if not out.is_contiguous() or out.numel() * out.element_size() != n_tok * rb_n:
         raise ValueError("out must be contiguous with n_tok * row_bytes bytes")
     if n_unique is not None and (n_unique.dtype != torch.int32 or n_unique.device.type != "cuda"):

@@ -106,3 +106,60 @@ def test_4bit_model_made_on_a_side_stream(as_handle):
         model = S.FgramModel(P, 512, 8, 1024, 2, 3)
         four = S.FgramModelMx4(model, stream=side.cuda_stream if as_handle else side)
         assert torch.equal(four.weights, want) and owner(four.weights) == side.cuda_stream
+
+
+def byte_inputs():
+    from gpu_util import build_gpu
+    rng = np.random.default_rng(5)
+    fg = np.unique(rng.integers(0, 30, (400, 3)), axis=0).astype(np.int32)
+    table = build_gpu(fg, np.full(len(fg), 3), np.arange(30, 30 + len(fg)))
+    g = torch.Generator("cuda").manual_seed(6)
+    rows = torch.randn((30 + len(fg), 256), generator=g, device="cuda")
+    tok = torch.randint(0, 30, (20, 100), generator=g, device="cuda").int()
+    torch.cuda.synchronize()
+    return table, rows, tok
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_results_of_the_byte_calls_live_on_their_stream(as_handle):
+    table, rows, tok = byte_inputs()
+    side = torch.cuda.Stream()
+    st = side.cuda_stream if as_handle else side
+    far = S.HostRows(rows.shape[0] - 30, (256,), torch.float32)
+    far.tensor().copy_(rows[30:])
+    ws = torch.empty(S.split_workspace_bytes(tok.numel(), 1024), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    ids, lens = S.lookup(table, tok, 3, want_len=True, stream=st)
+    results = [ids, lens, S.tag(table, tok, 3, stream=st)[0], S.gather(ids, rows, stream=st),
+               S.embed(table, tok, 3, rows, stream=st),
+               S.embed_pipelined(table, None, 3, None, ids, rows, stream=st),
+               S.gather_split(ids, rows[:30], far, ws, stream=st),
+               *S.discover_fgrams(tok, 3, 50, 2, stream=st)]
+    count = S.scone.lookup_counted(table, tok, 3, stream=st)
+    results += count[:2]
+    side.synchronize()
+    assert [owner(t) for t in results] == [side.cuda_stream] * len(results)
+    want, wlen = S.lookup(table, tok, 3, want_len=True)
+    again = S.scone.lookup_counted(table, tok, 3)
+    assert torch.equal(ids, want) and torch.equal(lens, wlen) and torch.equal(results[2], wlen)
+    assert torch.equal(count[0], want) and torch.equal(count[1], wlen) and count[2] == again[2] > 0
+    values = rows[want.long()]
+    assert all(torch.equal(t, values) for t in results[3:7])
+    assert S.check() == S.scone.OK
+    far.close()
+
+
+def test_chain_of_dropped_ids():
+    """A lookup whose ids are dropped behind the gather, on a side stream, under a busy
+    current one."""
+    table, rows, tok = byte_inputs()
+    want = S.embed(table, tok, 3, rows)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for _ in range(20):
+            for n in (tok.numel() * 4, tok.numel() * 1024):
+                torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+        got = S.gather(S.lookup(table, tok, 3, stream=side)[0], rows, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want)

@@ -146,3 +146,76 @@ def test_4bit_model_waits_for_the_model_it_is_made_from(gpu, stream):
     assert [h for s in made for h in s.waits] == [5]
     gpu.launched.clear()
     assert S.FgramModelMx4(model).weights.on == 5 and gpu.launched[0][1] == 5
+
+
+# ------------------------------------------------------- rows of any bytes ----
+
+def tokens(gpu):
+    return gpu.tensor(3, 20, dtype=torch.int32)
+
+
+TABLE = types.SimpleNamespace(handle=ctypes.c_void_p(64), device=torch.device("cuda", 0))
+
+
+def lookup(gpu, stream):
+    return S.lookup(TABLE, tokens(gpu), 3, want_len=True, stream=stream)
+
+
+def tag(gpu, stream):
+    return S.tag(TABLE, tokens(gpu), 3, stream=stream)[:1]
+
+
+def discover(gpu, stream):
+    gpu.monkeypatch.setattr(ctypes, "c_int64", lambda f=ctypes.c_int64: f(4))
+    return S.discover_fgrams(tokens(gpu), 3, 4, stream=stream)
+
+
+def gather_bytes(gpu, stream):
+    return [S.gather(tokens(gpu), gpu.tensor(9, 16, dtype=torch.float32), stream=stream)]
+
+
+def embed(gpu, stream):
+    return [S.embed(TABLE, tokens(gpu), 3, gpu.tensor(9, 16, dtype=torch.float32), stream=stream)]
+
+
+def embed_pipelined(gpu, stream):
+    return [S.embed_pipelined(TABLE, None, 3, None, tokens(gpu),
+                              gpu.tensor(9, 16, dtype=torch.float32), stream=stream)]
+
+
+def gather_split(gpu, stream):
+    far = S.HostRows.__new__(S.HostRows)
+    far.device_ptr, far.n_rows, far.row_bytes, far.row_shape = 4096, 9, 64, (16,)
+    far.dtype, far._closed = torch.float32, True
+    return [S.gather_split(tokens(gpu), gpu.tensor(9, 16, dtype=torch.float32), far,
+                           gpu.tensor(1 << 16, dtype=torch.uint8), stream=stream)]
+
+
+@pytest.mark.parametrize("call", [lookup, tag, discover, gather_bytes, embed, embed_pipelined,
+                                  gather_split], ids=lambda f: f.__name__)
+@pytest.mark.parametrize("kind", ["none", "current", "current handle", "other", "other handle"])
+def test_results_of_the_byte_calls(gpu, call, kind):
+    stream, handle = {"none": (None, 5), "current": (gpu.current, 5), "current handle": (5, 5),
+                      "other": (Stream(8), 8), "other handle": (8, 8)}[kind]
+    results = call(gpu, stream)
+    assert [h for _, h in gpu.launched] == [handle]
+    assert gpu.taken and all(t.on == handle for t in gpu.taken)
+    assert [t.also for t in gpu.taken] == [None if handle == 5 else 5] * len(gpu.taken)
+    assert len(results) > 0
+
+
+@pytest.mark.parametrize("kind", ["none", "other", "other handle"])
+def test_count_is_cleared_and_read_on_the_launch_stream(gpu, kind):
+    stream, handle = {"none": (None, 5), "other": (Stream(8), 8), "other handle": (8, 8)}[kind]
+    cleared = []
+    real = torch.zeros
+
+    def zeros(*size, dtype=None, device=None):
+        cleared.append(gpu.current.cuda_stream)
+        return real(*size, dtype=dtype).as_subclass(Tensor)
+
+    tok = tokens(gpu)
+    gpu.monkeypatch.setattr(torch, "zeros", zeros)
+    S.scone.lookup_counted(TABLE, tok, 3, stream=stream)
+    assert [h for _, h in gpu.launched] == cleared == Tensor.read_on == [handle]
+    assert all(t.on == handle for t in gpu.taken) and len(gpu.taken) == 2
