@@ -104,7 +104,9 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
 // rows at one block and the other twelve at the same or the next, each in its own banks.
 constexpr int kFewWaves = 8, kFewAhead = 4;
 
-// Rounds in LDS at once for MT * 16 rows: 34 KiB, four workgroups a compute unit.
+// Rounds in LDS at once for MT * 16 rows: 34 KiB.  Registers bound the workgroups of a
+// compute unit to three (MT = 1, 2 of 16-bit types) or two; 64 registers, for a fourth,
+// spill and took 22.4 us where 84 take 20.9 (16 rows of 16,384 x 4,096).
 constexpr int few_rounds(int mt) { return 4 / mt; }
 
 // Codes and scale byte of a block of 32, elements e on of the K that begin at x[row].
@@ -151,7 +153,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __res
     constexpr int kLds = kQuantize ? kCodes + kChunk * kRows * 4 : 0;
     constexpr int kSums = kFewWaves * kRows * 64;
     __shared__ __attribute__((aligned(16))) uint8_t smem[kLds > kSums ? kLds : kSums];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    // Known to be one per wavefront: what depends on it branches as a whole (a matrix
+    // instruction takes no notice of lanes that are switched off).
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = block_index(block0) * 16;
     const int fr = lane & 15, q = lane >> 4;
     const int g = (int)groups(K), rb = (int)row_bytes(K);
