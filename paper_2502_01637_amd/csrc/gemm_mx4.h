@@ -105,26 +105,63 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[kPer16<kType>]) {
 constexpr int kFewWaves = 8, kFewAhead = 4;
 
 // Rounds in LDS at once for MT * 16 rows: 34 KiB.  Registers bound the workgroups of a
-// compute unit to three (MT = 1, 2 of 16-bit types) or two; 64 registers, for a fourth,
-// spill and took 22.4 us where 84 take 20.9 (16 rows of 16,384 x 4,096).
+// compute unit to three (up to 80: MT = 1, 2 of 16-bit types without kEnd) or two; 64, for
+// a fourth, spill: 22.4 us where 20.9 without (16 rows of 16,384 x 4,096).
 constexpr int few_rounds(int mt) { return 4 / mt; }
 
-// Codes and scale byte of a block of 32, elements e on of the K that begin at x[row].
+// Eight elements without the first d of them (d < 8), zeros behind.
 template <int kType>
+__device__ __forceinline__ typename Elem<kType>::vec drop(typename Elem<kType>::vec v, uint32_t d) {
+    constexpr int W = sizeof(v) / 4, kPerWord = 8 / W;  // words, elements in each
+#pragma unroll
+    for (int step = W / 2; step >= 1; step /= 2) {
+        const bool on = d & (step * kPerWord);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = on ? (i + step < W ? v[i + step] : 0u) : v[i];
+    }
+    if constexpr (kPerWord == 2) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            v[i] = d & 1 ? (v[i] >> 16) | (i + 1 < W ? v[i + 1] << 16 : 0u) : v[i];
+    }
+    return v;
+}
+
+// Codes and scale byte of a block of 32, elements e on of the K that begin at x[row].
+// kEnd: K is no multiple of 32.  Eights that pass the row's end are loaded from K - 8 on
+// and moved, so that every lane has its loads on their way at once: element by element,
+// behind a branch, 16 rows of 4,001 x 1,500 took 6.7 us, now 5.1 (K = 1,536 4.4), 32 rows
+// 9.1 and 7.1.  It needs 17 to 41 registers more, so whole blocks have kernels without it,
+// where a branch keeps the loads from being moved further up, which costs as many.
+template <int kType, bool kEnd>
 __device__ __forceinline__ u32x4 quantize32(const void* __restrict__ x, int64_t row, int64_t e,
                                             int64_t K, uint32_t& s) {
     typedef Elem<kType> E;
     const typename E::type* p = static_cast<const typename E::type*>(x) + row;
     typename E::vec v[4];
-    if (e + 32 <= K) {
+    if constexpr (!kEnd) {
+        if (e + 32 <= K) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = load8<kType>(p + e + i * 8, 8);
-    } else {
+            for (int i = 0; i < 4; ++i) v[i] = load8<kType>(p + e + i * 8, 8);
+        } else {
+            for (int i = 0; i < 4; ++i) v[i] = typename E::vec{};
+        }
+    } else if (K >= 8) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t left = K - e - i * 8;
-            v[i] = load8<kType>(p + (left > 0 ? e + i * 8 : 0), left);
+            const int64_t from = e + i * 8;
+            v[i] = load8<kType>(p + (from < K - 8 ? from : K - 8), 8);
         }
+        if (e + 32 > K) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t d = e + i * 8 - (K - 8);
+                if (d > 0) v[i] = d < 8 ? drop<kType>(v[i], (uint32_t)d) : typename E::vec{};
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = load8<kType>(p, e + i * 8 == 0 ? K : 0);
     }
     uint32_t top = 0;
 #pragma unroll
@@ -139,7 +176,7 @@ __device__ __forceinline__ u32x4 quantize32(const void* __restrict__ x, int64_t 
     return codes;
 }
 
-template <int kType, int MT>
+template <int kType, int MT, bool kEnd>
 __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __restrict__ x,
                                                                int64_t ld,
                                                                const uint8_t* __restrict__ w,
@@ -183,7 +220,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __res
             for (int u = threadIdx.x; u < (int)ep.M * n; u += 64 * kFewWaves) {
                 const int r = u / n, c = u - r * n, k = c >> 2;
                 uint32_t s;
-                const u32x4 codes = quantize32<kType>(x, r * ld, (int64_t)(k0 * 4 + c) * 32, K, s);
+                const u32x4 codes = quantize32<kType, kEnd>(x, r * ld, (int64_t)(k0 * 4 + c) * 32, K, s);
                 const int slot = (c & 3) ^ (-(r >> 2) & 3);
                 *reinterpret_cast<u32x4*>(smem + (k * kRows + r) * 64 + slot * 16) = codes;
                 smem[kCodes + (k * kRows + r) * 4 + (c & 3)] = (uint8_t)s;
@@ -247,13 +284,21 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const void* __res
     }
 }
 
-template <int kType, int MT>
+template <int kType, int MT, bool kEnd>
 inline hipError_t launch_few(const void* x, int64_t ld, const uint8_t* w, int64_t K,
                              const Epilogue& ep, hipStream_t st) {
     return launch_blocks((ep.N + 15) / 16, 64 * kFewWaves, [&](int64_t b0, dim3 grid) {
-        hipLaunchKernelGGL((k_linear_few<kType, MT>), grid, dim3(64 * kFewWaves), 0, st, x, ld, w,
-                           K, ep, b0);
+        hipLaunchKernelGGL((k_linear_few<kType, MT, kEnd>), grid, dim3(64 * kFewWaves), 0, st, x,
+                           ld, w, K, ep, b0);
     });
+}
+
+template <int kType, int MT>
+inline hipError_t launch_few(const void* x, int64_t ld, const uint8_t* w, int64_t K,
+                             const Epilogue& ep, hipStream_t st) {
+    if constexpr (kType != SCONE_MX4)
+        if (K % 32 != 0) return launch_few<kType, MT, true>(x, ld, w, K, ep, st);
+    return launch_few<kType, MT, false>(x, ld, w, K, ep, st);
 }
 
 template <int kType>
