@@ -711,7 +711,7 @@ bool sizes_ok(int64_t M, int64_t N, int64_t K) {
 extern "C" int64_t scone_linear_mx4_workspace(int64_t M, int64_t N, int64_t K, int32_t x_type) {
     using namespace scone;
     if (!sizes_ok(M, N, K) || (x_type != SCONE_MX4 && mx4::elem_bytes(x_type) == 0)) return -1;
-    return mx4::linear_workspace(M, N, K);
+    return mx4::linear_workspace(M, N, K, x_type);
 }
 
 extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int64_t M, int64_t K,
@@ -739,7 +739,7 @@ extern "C" int scone_linear_mx4(const void* x, int32_t x_type, int64_t ld_x, int
     // them, except the residual, which each element reads before it is written, where
     // it is the output itself.
     const int64_t out_b = ((M - 1) * ld_out + N) * oe;
-    const int64_t need = mx4::linear_workspace(M, N, K);
+    const int64_t need = mx4::linear_workspace(M, N, K, x_type);
     const void* buf[5] = {x, w, bias, residual, workspace};
     const int64_t len[5] = {packed ? M * rb : ((M - 1) * ld_x + K) * xe, N * rb, N * be, out_b,
                             need};

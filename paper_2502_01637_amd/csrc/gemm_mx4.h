@@ -773,21 +773,29 @@ inline hipError_t launch_tiles(const Slabs& x, const Slabs& w, int64_t K, const 
     }
 }
 
-// Whether a product takes the tiles.  k_linear_few quantises x again in every workgroup,
-// so from 17 rows on it pays as long as that is little: blocks of 16 rows of x by groups,
-// up to 64 in a workgroup and 8,192 in all.  Against the tiles, us, at 16, 32 and 64 rows:
-// N 4,096, K 1,024 3.7, 4.6, 6.9 and 8.3, 8.9, 8.5; 4,001 x 1,500 6.3, 8.7, 11.1 and 9.8,
-// 10.4, 10.5; 1,024 x 4,096 6.9, 10.1, 17.1 and 13.5, 14.0, 13.3; 16,384 x 4,096 19.4,
-// 27.9, 49.9 and 25.3, 25.7, 25.0.
-inline bool tiled(int64_t M, int64_t N, int64_t K) {
-    if (M <= 16) return false;
-    const int64_t blocks = (M <= 32 ? 2 : 4) * groups(K);
-    return M > 64 || blocks > 64 || blocks * ((N + 15) / 16) > 8192;
+// Whether a product takes the tiles.  Up to 64 rows k_linear_few has one launch and no
+// layout of w, but every workgroup brings all rows of x to 4 bits again, or reads their
+// codes.  Rows count by what that costs (4-bit 1, 16-bit 2, fp32 4), and the more there
+// are, the fewer groups and workgroups it pays for.  Us, k_linear_few / tiles:
+//   N x K            4-bit x, M = 32, 64     bf16, M = 16, 32, 64           fp32, M = 16, 32
+//   4,096 x 1,024    3.9/8.7  5.0/8.4        4.0/8.7  5.0/8.9   7.2/9.0     5.2/9.2  7.2/9.3
+//   4,001 x 1,500    4.1/10.6 5.6/10.5       5.2/10.2 7.2/10.8 10.3/11.3             10.1/10.8
+//   1,024 x 4,096    8.0/13.3 12.0/13.2      7.4/13.7 10.8/13.9 18.0/13.8  11.8/14.0 19.8/14.3
+//   16,384 x 1,024   6.7/12.8 11.1/12.6               9.4/12.8  16.8/12.7  12.3/12.6 19.2/13.1
+//   8,192 x 4,096    14.0/21.0 22.4/21.4              17.7/21.4 30.0/21.2  21.4/21.1
+//   16,384 x 4,096   25.3/27.2 48.6/26.6    21.0/27.5 30.2/26.8 53.6/26.7  39.4/27.8
+inline bool tiled(int64_t M, int64_t N, int64_t K, int32_t type) {
+    if (M > 64) return true;
+    const int64_t rows = M * (type == SCONE_MX4 ? 1 : type == SCONE_FP32 ? 4 : 2);
+    const int64_t g = groups(K), workgroups = (N + 15) / 16;
+    return rows <= 32   ? false
+           : rows <= 64 ? g * workgroups > 16384
+                        : rows > 128 || g > 16 || workgroups > 512;
 }
 
 // Scratch of a linear map: the slabs of x and w.
-inline int64_t linear_workspace(int64_t M, int64_t N, int64_t K) {
-    return tiled(M, N, K) && N > 0 ? slabs_bytes(M, K) + slabs_bytes(N, K) : 0;
+inline int64_t linear_workspace(int64_t M, int64_t N, int64_t K, int32_t type) {
+    return tiled(M, N, K, type) && N > 0 ? slabs_bytes(M, K) + slabs_bytes(N, K) : 0;
 }
 
 template <int kType>
@@ -803,7 +811,7 @@ inline hipError_t launch_slabs(const void* x, int64_t ld, const Slabs& sx, const
 // x: 4-bit rows, or (type not SCONE_MX4) rows to quantise.
 inline hipError_t linear(const void* x, int32_t type, int64_t ld, const uint8_t* w, int64_t K,
                          const Epilogue& ep, uint8_t* ws, hipStream_t st) {
-    if (!tiled(ep.M, ep.N, K)) {
+    if (!tiled(ep.M, ep.N, K, type)) {
         switch (type) {
             case SCONE_BF16: return launch_few<SCONE_BF16>(x, ld, w, K, ep, st);
             case SCONE_FP16: return launch_few<SCONE_FP16>(x, ld, w, K, ep, st);

@@ -10,9 +10,9 @@ pytestmark = pytest.mark.gpu
 WIDTHS = list(range(1, 140)) + [255, 256, 257, 383, 500, 1000, 1023, 1025, 1500, 2047, 4100]
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
-@pytest.mark.parametrize("M", [1, 5, 16, 19, 33])
-def test_rows_are_quantised_as_by_quantize_mx4(dtype, M):
+@pytest.mark.parametrize("M,dtype", [(M, t) for t in (torch.bfloat16, torch.float16, torch.float32)
+                                     for M in (1, 5, 16, 19, 32, 33) if M <= 32 or t.itemsize == 2])
+def test_rows_are_quantised_as_by_quantize_mx4(M, dtype):
     """Both sides sum in the same order, so that equal codes give equal results; what
     lies around the rows is NaN."""
     for K in [K for K in WIDTHS if M <= 16 or K <= 2048]:   # beyond, tiles take them
@@ -26,3 +26,20 @@ def test_rows_are_quantised_as_by_quantize_mx4(dtype, M):
         got = S.linear_mx4(x, w, dtype=torch.float32)
         assert torch.equal(got, S.linear_mx4(S.quantize_mx4(x), w, dtype=torch.float32)), K
         assert torch.isfinite(got).all(), K
+
+
+@pytest.mark.parametrize("M", [9, 16, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("N,K", [(1024, 4100), (4001, 1500), (8300, 2100), (16400, 500)])
+@pytest.mark.parametrize("dtype", [None, torch.bfloat16, torch.float32])
+def test_both_sides_of_the_row_limits(M, N, K, dtype):
+    """Products whose sums no order of adding rounds, whichever kernel takes them: x of
+    whole numbers up to 6 (one scale), w of halves and scales of 1."""
+    g = torch.Generator("cuda").manual_seed(M + K)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda")
+    x, w = (grid[torch.randint(0, 8, (n, K), generator=g, device="cuda")]
+            * (torch.randint(0, 2, (n, K), generator=g, device="cuda") * 2 - 1) for n in (M, N))
+    x[:, ::32], w[:, ::32] = 6.0, 4.0          # every block's largest: scale 1
+    xin = S.quantize_mx4(x) if dtype is None else x.to(dtype)
+    got = S.linear_mx4(xin, S.quantize_mx4(w), dtype=torch.float32)
+    assert 36 * K < 2 ** 22                    # multiples of 1/4 below 2^22: 24 bits
+    assert torch.equal(got.double(), x.double() @ w.double().t())
