@@ -828,14 +828,20 @@ inline hipError_t linear(const void* x, int32_t type, int64_t ld, const uint8_t*
         default: e = launch_slabs<SCONE_MX4>(x, ld, sx, w, sw, K, ep, st);
     }
     if (e != hipSuccess) return e;
-    // The large tiles from one a compute unit on, the small ones below, of which there
-    // are four times as many.  Us, large and small, at 96, 192, 256, 512 and 1,024 large
-    // tiles: N 4,096, K 1,024 12.2, 14.0, 15.4, 23.0, 34.9 and 11.8, 14.1, 15.9, 24.1, 39.1;
-    // N 16,384, K 4,096 (from 128 on) 31.8, 33.2, 36.6, 53.1, 86.6 and 30.0, 36.5, 41.8,
-    // 65.6, 115.
+    // The small tiles, four for a large one, as long as they run in one round (three a
+    // compute unit, 768); over a long loop the large ones from two small ones a compute
+    // unit on.  Us, large / small, at 128, 160, 192, 224, 256 and 512 large tiles:
+    //   4,096 x 1,024         14.7/13.7 15.6/15.6 16.1/16.2 16.7/17.9 17.4/18.4 25.4/27.5
+    //   the same, GELU        18.6/15.0 19.4/17.2 19.8/17.8 20.3/20.2 21.0/20.5 29.8/31.0
+    //   4,096 x 2,048         20.3/20.2 21.7/23.1 22.3/23.6 23.6/26.8 24.9/27.4
+    //   the same, GELU        24.3/20.9 25.5/24.8 26.2/25.2 27.5/28.6 28.7/29.5
+    //   2,048 x 2,048, fp32 residual 24.6/20.8 24.1/23.1 25.6/24.0 27.9/29.1 28.9/28.6
+    //   4,096 x 4,096, GELU   32.9/28.7 32.2/33.8 33.4/34.9 35.3/39.8 37.1/41.1
+    //   1,024 x 4,096, fp32 residual 32.5/28.5 34.8/35.4 37.6/37.9 40.8/43.9 44.3/47.2 77.0/86.3
+    //   16,384 x 4,096        34.4/33.5           36.7/40.0           39.8/46.0 58.2/71.4
     const int64_t big = ((ep.M + 127) / 128) * ((ep.N + 255) / 256);
-    return big >= 256 ? launch_tiles<2, 4>(sx, sw, K, ep, st)
-                      : launch_tiles<1, 2>(sx, sw, K, ep, st);
+    return big > (groups(K) < 32 ? 192 : 128) ? launch_tiles<2, 4>(sx, sw, K, ep, st)
+                                              : launch_tiles<1, 2>(sx, sw, K, ep, st);
 }
 
 }  // namespace mx4

@@ -43,3 +43,20 @@ def test_both_sides_of_the_row_limits(M, N, K, dtype):
     got = S.linear_mx4(xin, S.quantize_mx4(w), dtype=torch.float32)
     assert 36 * K < 2 ** 22                    # multiples of 1/4 below 2^22: 24 bits
     assert torch.equal(got.double(), x.double() @ w.double().t())
+
+
+@pytest.mark.parametrize("M,N,K", [(1530, 4000, 1100), (1600, 4000, 1100), (1020, 4001, 4100),
+                                   (1100, 4001, 4100), (12000, 520, 300), (8300, 1000, 200)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_both_sides_of_the_tile_limits(M, N, K, residual):
+    """As above, around 192 and (over a long K) 128 large tiles."""
+    g = torch.Generator("cuda").manual_seed(M + K)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda")
+    x, w = (grid[torch.randint(0, 8, (n, K), generator=g, device="cuda")]
+            * (torch.randint(0, 2, (n, K), generator=g, device="cuda") * 2 - 1) for n in (M, N))
+    x[:, ::32], w[:, ::32] = 6.0, 4.0
+    bias = torch.randint(-8, 9, (N,), generator=g, device="cuda").float()
+    res = torch.randint(-99, 99, (M, N), generator=g, device="cuda").float() if residual else None
+    got = S.linear_mx4(x, S.quantize_mx4(w), bias, residual=res)
+    want = x.double() @ w.double().t() + bias.double()
+    assert torch.equal(got.double(), want if res is None else want + res.double())
