@@ -596,7 +596,8 @@ int64_t scone_fgram_model_workspace(int64_t n, int32_t max_len, int32_t d, int32
  *  params    as there; its linear weights are not read.
  *  weights   scone_fgram_model_mx4_bytes bytes, 16-byte aligned: per layer the 4-bit
  *            rows of w_qkv [3d], w_o [d], w_fc1 [d_ff] and w_fc2 [d], one after another,
- *            as scone_fgram_model_quantize writes them from params.  Sharing memory with
+ *            as scone_fgram_model_quantize writes them from params (NULL where there
+ *            are no layers, which have none).  Sharing memory with
  *            rows or the workspace gives SCONE_EINVAL.
  *  workspace at least scone_fgram_model_workspace_mx4 bytes, or NULL.
  *

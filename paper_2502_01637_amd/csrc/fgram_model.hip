@@ -643,7 +643,7 @@ extern "C" int scone_fgram_model_forward_mx4(const int32_t* fgrams, const int32_
                                              int32_t n_heads, int32_t d_ff, int32_t n_layers,
                                              void* rows, int64_t n_rows, void* workspace,
                                              int64_t workspace_bytes, void* stream) {
-    if (!weights && n != 0) return SCONE_EINVAL;
+    if (!weights && n != 0 && n_layers != 0) return SCONE_EINVAL;
     return scone::forward_in(fgrams, lengths, row_ids, n, max_len, tok_rows, vocab, params,
                              weights, d, n_heads, d_ff, n_layers, rows, n_rows, workspace,
                              workspace_bytes, stream);
