@@ -1451,7 +1451,7 @@ def reduce_precompute(trace_csv, bench_json, pmc_csv, out_md, trace_cmd, pmc_cmd
     pf = bench["product_flops_per_step"]
     L.append(f"Matrix products: {pf / 1e12:.1f} TFLOP of work per call (the states of shared "
              f"prefixes counted once) in "
-             f"{prod_ns / 1e6:.1f} ms of {'their kernels' if four else 'k_gemm'} time, "
+             f"{prod_ns / 1e6:.1f} ms of {'kernel' if four else 'k_gemm'} time, "
              f"{pf / prod_ns / 1e3:.0f} TFLOP/s ({100 * pf / prod_ns / 1e3 / peak:.1f}% of the "
              f"{peak / 1000:g} PFLOP/s dense {'4-bit' if four else 'bf16'} peak).  "
              f"Whole call: {bench['flops_per_step'] / 1e12:.1f} TFLOP in {all_ns / 1e6:.1f} ms "

@@ -661,8 +661,9 @@ __global__ __launch_bounds__(256, workgroups(TM, TN)) void k_linear_tiles(
     __builtin_amdgcn_sched_barrier(0);
     uint8_t* const part = smem + wave * 32 * PITCH;
     // kInside, kGelu: known (0, 1) or looked up (2).  Known, the way out is straight code
-    // that reads the next sums while others leave (280 -> 269 us for 65,459 x 4,096 x
-    // 1,024 with GELU).  With residuals that was slower (196 -> 216 us, x 1,024 x 4,096):
+    // that reads the next sums while others leave (65,459 x 4,096 x 1,024 with GELU 287 ->
+    // 279 us, to fp32 320 -> 303; without it 65,459 x 4,096 x 512 157 -> 147, x 1,024 231 ->
+    // 235).  With residuals that was slower (196 -> 216 us, x 1,024 x 4,096):
     // more of them in flight hold up the copies of the other workgroup.
     // In tiles over an edge the lanes whose columns are all there still move 16 bytes
     // (by elements 1,000 x 16,384 x 4,096 took 58.7 us, now 50.2).
